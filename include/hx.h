@@ -28,6 +28,13 @@
  *   hx_spectral_order        the Fiedler order of the device graph  (one workgroup)
  *   hx_partition_candidates  partition, swaps, role split per draw  (a wavefront or workgroup per candidate)
  *
+ * and what a search or a coordinator does with scored placements:
+ *
+ *   hx_sample          one entry drawn from every row of scores   (a workgroup or more per row)
+ *   hx_route_requests  requests drawn along the flow assignment   (one lane per request)
+ *   hx_kv_place        KV blocks and token slots of those requests (one lane per row, then per token)
+ *   hx_kv_release      their blocks back to the free lists
+ *
  * Conventions
  *   - Every array pointer is a DEVICE pointer unless marked [host].  The caller owns every
  *     buffer; libhx allocates no device memory and keeps no state between calls.
@@ -423,21 +430,138 @@ int hx_partition_candidates(const hx_cluster *cluster, hx_model model, hx_worklo
                             void *workspace, size_t workspace_bytes, const int32_t *order, int32_t n_cand,
                             const uint64_t *rnd, uint8_t *assign, uint8_t *role, hipStream_t stream);
 
+/* ---------------------------------------------------------------- drawing from scored rows
+ * The draw beside hx_best_candidate's argmax: one entry of every row of scores, with probability
+ * proportional to exp(score / temperature) among the entries that top-k, top-p and min-p keep.  A
+ * row holds a batch's flow values (a refinement chain that draws its next parent instead of always
+ * taking the best leaves local maxima, Sec. 3.4) or the logits of one sequence of a decode replica. */
+#define HX_SCORE_I32 0
+#define HX_SCORE_F32 1
+#define HX_SCORE_F16 2
+#define HX_SCORE_BF16 3
+typedef struct hx_scores {
+    int32_t n_rows, n_cols;     /* R >= 1, N >= 1 */
+    int32_t type;               /* HX_SCORE_* */
+    int64_t row_stride;         /* elements from one row to the next, >= 0 (0: every row reads the same scores) */
+    const void *data;           /* [R][row_stride], aligned to its element */
+} hx_scores;
+
+/* Per-row parameters, device arrays of R; a null pointer turns the filter off (temperature: 1). */
+typedef struct hx_sampling {
+    const float *temperature;   /* T, finite and >= 0; 0: the highest score, lowest index on ties */
+    const int32_t *top_k;       /* k >= 1; <= 0: off */
+    const float *top_p;         /* p; >= 1: off */
+    const float *min_p;         /* q; <= 0: off */
+} hx_sampling;
+
+/* One draw per row.  NaN, -inf and INT32_MIN are masked.  Of a row's other scores x_i, m the largest,
+ *   z_i = 0 where x_i == m, else (x_i - m) / T,  w_i = exp(z_i), in binary64;
+ *   ordered by descending score, ascending index on ties, the row keeps its first
+ *   min(K, P, Q) entries, at least one: K = k (or all); P the fewest entries whose weights reach
+ *   p times the weight of the first K; Q the number of entries with w_i >= q;
+ *   S is the weight of the kept entries, t = ((rnd >> 11) / 2^53) S, and the pick is the first kept
+ *   entry, in ascending index, up to which the kept weights sum to more than t.
+ * Every sum is taken in binary64 or in whole numbers of 2^-s, s as large as 64 bits allow, in an order
+ * that does not depend on the launch's timing.
+ *   rnd  [R] uniform 64-bit draws;
+ *   pick [R] the index drawn; logp [R] nullable: z_pick - log S; kept [R] nullable: min(K, P, Q).
+ * T = 0 gives the argmax, logp 0, kept 1.  A row that masks everything, or whose T is negative or not
+ * finite, or whose p or q is NaN, gets pick -1, logp -inf, kept 0.
+ *   workspace: hx_sample_workspace_bytes(R, N) bytes (0 for sizes below 1), 256-byte aligned, contents
+ *   ignored on entry; calls that share it must not overlap. */
+size_t hx_sample_workspace_bytes(int32_t n_rows, int32_t n_cols);
+int hx_sample(const hx_scores *scores, const hx_sampling *params, const uint64_t *rnd, int32_t *pick, float *logp,
+              int32_t *kept, void *workspace, size_t workspace_bytes, hipStream_t stream);
+
+/* ---------------------------------------------------------------- dispatch (Sec. 3.3, 4)
+ * From a placement's flow assignment to its replicas' memory: Sec. 3.3 sends requests' KV caches along an
+ * edge at a rate proportional to its flow, and a replica holds them in blocks of its paged KV memory. */
+
+/* Routes of n_req requests: node indices of the network, and each node's requests.  Each pair of order
+ * and base may be null: order holds the request numbers grouped by node, ascending within a node (those
+ * without a route last), base[k] where node k's run starts, base[max_p] (base[max_d]) their total. */
+typedef struct hx_routes {
+    int32_t n_req;              /* >= 1 */
+    int32_t *prefill, *decode;  /* [n_req], -1: no route */
+    int32_t *p_order, *p_base;  /* [n_req], [max_p + 1] */
+    int32_t *d_order, *d_base;  /* [n_req], [max_d + 1] */
+} hx_routes;
+
+/* One KV edge per request, drawn in proportion to its flow: with F the sum of column cand of kv_flow over
+ * the network's edges i*n_d + j (negative entries count 0), request r takes the first edge up to which the
+ * flows sum to more than floor(rnd[r] F / 2^64).  F = 0, or counts outside the arrays (n_p > max_p, n_d >
+ * max_d, n_p*n_d > max_pd, negative): no request gets a route.  Whole numbers throughout.  max_p, max_d <=
+ * HX_MAX_GPUS, cand in [0, net->n_cand); of net only the counts are read.
+ *   rnd [n_req] uniform 64-bit draws; workspace as for hx_sample. */
+size_t hx_route_workspace_bytes(int32_t max_p, int32_t max_d, int32_t max_pd, int32_t n_req);
+int hx_route_requests(const hx_flownet *net, int32_t cand, const int32_t *kv_flow, const uint64_t *rnd,
+                      const hx_routes *out, void *workspace, size_t workspace_bytes, hipStream_t stream);
+
+/* Paged KV memory of n_replicas replicas: replica r's free blocks are the first free_count[r] entries of
+ * free_list[base[r] .. base[r + 1]), taken from their end and given back to it. */
+typedef struct hx_kv_pool {
+    int32_t n_replicas;         /* 1..255 */
+    int32_t block_size;         /* tokens per block, 1..65536 */
+    const int32_t *base;        /* [n_replicas + 1], ascending from >= 0 */
+    int32_t *free_list;         /* [base[n_replicas]] block numbers, the replica's own numbering */
+    const int32_t *free_count;  /* [n_replicas] (clamped to the replica's range) */
+    int32_t *free_out;          /* [n_replicas] the counts after the call; may be free_count itself */
+} hx_kv_pool;
+
+/* Rows of a serving batch: row i's KV cache lives on replica[i] (outside [0, n_replicas): nowhere) and
+ * holds held[i] tokens in the blocks block_table[i][0 .. ceil(held[i] / block_size)). */
+typedef struct hx_kv_rows {
+    int32_t n_rows;             /* >= 1 */
+    int32_t max_blocks;         /* usable columns of a row, >= 1 */
+    int64_t table_stride;       /* elements from one row to the next, >= max_blocks */
+    int32_t *block_table;
+    const int32_t *replica;     /* [n_rows] */
+    const int32_t *held;        /* [n_rows] */
+    int32_t *held_out;          /* [n_rows] the lengths after the call; may be held itself */
+} hx_kv_rows;
+
+/* Memory for n_new[i] more tokens of every row: a prompt, a chunk of one, or the next token of a decode
+ * step.  A row needs ceil((held + n_new) / b) - ceil(held / b) blocks, b = block_size; rows of one replica
+ * are served in ascending order until the first whose blocks the replica does not have, and from there
+ * only rows that need none.  The row that is served takes the top of its replica's free list, block by
+ * block, into its next table columns; its token t gets slot block * b + (held + t) mod b.
+ *   tok_base [n_rows + 1]: sum of n_new over the rows before (a negative n_new counts 0);
+ *   slots  [max_slots]: row i's tokens at tok_base[i]; -1 for those of a row not served; entries past the
+ *          last token are left as they were;
+ *   placed [n_rows]: 1 where served, held_out = held + n_new there and held elsewhere.
+ * Not served: rows on no replica, with held or n_new negative, past max_blocks columns or 2^31 - 1 tokens,
+ * or whose tokens end past max_slots.  Table columns that gain no block are left as they were.
+ *   workspace: hx_kv_workspace_bytes(n_rows, n_replicas), 256-byte aligned, contents ignored on entry;
+ *   calls that share it must not overlap. */
+size_t hx_kv_workspace_bytes(int32_t n_rows, int32_t n_replicas);
+int hx_kv_place(const hx_kv_pool *pool, const hx_kv_rows *rows, const int32_t *n_new, int64_t *tok_base,
+                int64_t *slots, int64_t max_slots, uint8_t *placed, void *workspace, size_t workspace_bytes,
+                hipStream_t stream);
+
+/* The blocks of every row with done[i] != 0 back to its replica, held_out 0 there: the last row's last block
+ * first, so that releasing the rows that one hx_kv_place served on empty caches leaves the free lists as they
+ * were.  Tables keep their entries.  Rows on no replica, with held negative or past max_blocks columns, or
+ * whose blocks would not fit the replica's range, are left alone. */
+int hx_kv_release(const hx_kv_pool *pool, const hx_kv_rows *rows, const uint8_t *done, void *workspace,
+                  size_t workspace_bytes, hipStream_t stream);
+
 /* Diagnostic per-kernel timing (not part of the scoring path; process-global, for one host
  * thread).  hx_profile(1) clears earlier records and makes every later launch by libhx record a
  * HIP event on the call's stream before and after each of its kernels; hx_profile(0) stops
  * recording.  hx_profile_read waits for the recorded events and fills ms[k] (total
  * milliseconds) and launches[k] for kernel k = 0 .. n-1 since the last hx_profile call, then
- * clears the records; n >= HX_KERNELS.  Returns HX_KERNELS or a negative error.  hx_kernel_name
+ * clears the records; n >= HX_KERNELS, or from 14 up for the first n kernels alone.  Returns the number of
+ * kernels filled or a negative error.  hx_kernel_name
  * gives kernel k's name: setup, decode, scatter, eval (hx_cost_eval), nodes, kv
  * (hx_build_flownet), maxflow, best, classes (hx_edge_classes), moves (hx_guided_moves),
  * gather (hx_gather_candidates), spectral (hx_spectral_order), partition
- * (hx_partition_candidates), shared (candidate 0's groups under HX_HINT_SHARED_GROUPS).  The
+ * (hx_partition_candidates), shared (candidate 0's groups under HX_HINT_SHARED_GROUPS), sample, route,
+ * place and release (hx_sample, hx_route_requests, hx_kv_place, hx_kv_release).  The
  * kernels that hx_score_batch joins have one name: on replica networks that one kernel builds and
  * settles, kv holds the nodes, KV edges and settled values, maxflow the listed networks and the
  * argmax, nodes and best nothing; on per-GPU networks kv is the table of links, nodes the nodes
  * and settled values. */
-#define HX_KERNELS 14
+#define HX_KERNELS 18
 int hx_profile(int32_t enable);
 int hx_profile_read(double *ms, int32_t *launches, int32_t n);
 const char *hx_kernel_name(int32_t k);

@@ -238,8 +238,10 @@ int hx_profile(int32_t enable) {
 }
 
 int hx_profile_read(double* ms, int32_t* launches, int32_t n) {
-    if (!ms || !launches || n < hx::kKCount) return HX_EINVAL;
-    for (int k = 0; k < hx::kKCount; ++k) {
+    constexpr int kFirst = 14;  // callers built when these were all the kernels
+    if (!ms || !launches || n < kFirst) return HX_EINVAL;
+    if (n > hx::kKCount) n = hx::kKCount;
+    for (int k = 0; k < n; ++k) {
         ms[k] = 0.0;
         launches[k] = 0;
     }
@@ -254,17 +256,19 @@ int hx_profile_read(double* ms, int32_t* launches, int32_t n) {
         hipError_t e = hipEventSynchronize(q.e);
         if (e == hipSuccess) e = hipEventElapsedTime(&t, q.b, q.e);
         if (e != hipSuccess) return hip_error(e);
+        if (q.k >= n) continue;
         ms[q.k] += t;
         launches[q.k] += 1;
     }
     prof_clear();
-    return hx::kKCount;
+    return n;
 }
 
 const char* hx_kernel_name(int32_t k) {
     static const char* names[hx::kKCount] = {"setup", "decode",  "scatter", "eval",     "nodes",
                                              "kv",    "maxflow", "best",    "classes",  "moves",
-                                             "gather", "spectral", "partition", "shared"};
+                                             "gather", "spectral", "partition", "shared",
+                                             "sample", "route",   "place",   "release"};
     return k >= 0 && k < hx::kKCount ? names[k] : "";
 }
 
@@ -518,6 +522,85 @@ int hx_gather_candidates(int32_t n_gpus, const hx_candidates* src, const int32_t
     if (!index || count < 1 || !dst_assign || !dst_role) return HX_EINVAL;
     hipError_t e = hx::launch_gather(n_gpus, src->max_groups, src->n_cand, src->assign, src->role, index, count,
                                      dst_assign, dst_role, stream);
+    return e == hipSuccess ? HX_OK : hip_error(e);
+}
+
+// ------------------------------------------------------------------ draws and dispatch
+
+size_t hx_sample_workspace_bytes(int32_t n_rows, int32_t n_cols) {
+    return n_rows < 1 || n_cols < 1 ? 0 : hx::sample_workspace_bytes(n_rows, n_cols);
+}
+
+int hx_sample(const hx_scores* scores, const hx_sampling* params, const uint64_t* rnd, int32_t* pick, float* logp,
+              int32_t* kept, void* workspace, size_t workspace_bytes, hipStream_t stream) {
+    if (!scores || !params || !rnd || !pick || !scores->data) return HX_EINVAL;
+    if (scores->n_rows < 1 || scores->n_cols < 1 || scores->row_stride < 0) return HX_EINVAL;
+    if (scores->type < HX_SCORE_I32 || scores->type > HX_SCORE_BF16) return HX_EINVAL;
+    const uintptr_t elem = scores->type == HX_SCORE_I32 || scores->type == HX_SCORE_F32 ? 4 : 2;
+    if ((uintptr_t)scores->data & (elem - 1)) return HX_EINVAL;
+    if (!workspace || ((uintptr_t)workspace & 255) ||
+        workspace_bytes < hx::sample_workspace_bytes(scores->n_rows, scores->n_cols))
+        return HX_EINVAL;
+    const hx::SampleArgs a{scores->n_rows, scores->n_cols, scores->type,  scores->row_stride, scores->data,
+                           params->temperature, params->top_p, params->min_p, params->top_k, rnd, pick, kept, logp};
+    hipError_t e = hx::launch_sample(a, workspace, stream);
+    return e == hipSuccess ? HX_OK : hip_error(e);
+}
+
+size_t hx_route_workspace_bytes(int32_t max_p, int32_t max_d, int32_t max_pd, int32_t n_req) {
+    if (max_p < 1 || max_p > HX_MAX_GPUS || max_d < 1 || max_d > HX_MAX_GPUS || max_pd < 1 || n_req < 1) return 0;
+    return hx::route_workspace_bytes(max_p, max_d, max_pd, n_req);
+}
+
+int hx_route_requests(const hx_flownet* net, int32_t cand, const int32_t* kv_flow, const uint64_t* rnd,
+                      const hx_routes* out, void* workspace, size_t workspace_bytes, hipStream_t stream) {
+    if (!net || net->n_cand < 1 || net->max_p < 1 || net->max_d < 1 || net->max_pd < 1 || !net->n_p || !net->n_d)
+        return HX_EINVAL;
+    if (net->max_p > HX_MAX_GPUS || net->max_d > HX_MAX_GPUS || cand < 0 || cand >= net->n_cand) return HX_EINVAL;
+    if (!kv_flow || !rnd || !out || out->n_req < 1 || !out->prefill || !out->decode) return HX_EINVAL;
+    if (!out->p_order != !out->p_base || !out->d_order != !out->d_base) return HX_EINVAL;
+    if (!workspace || ((uintptr_t)workspace & 255) ||
+        workspace_bytes < hx::route_workspace_bytes(net->max_p, net->max_d, net->max_pd, out->n_req))
+        return HX_EINVAL;
+    hipError_t e = hx::launch_route(make_net(net), cand, kv_flow, rnd, *out, workspace, stream);
+    return e == hipSuccess ? HX_OK : hip_error(e);
+}
+
+size_t hx_kv_workspace_bytes(int32_t n_rows, int32_t n_replicas) {
+    return n_rows < 1 || n_replicas < 1 || n_replicas > 255 ? 0 : hx::kv_workspace_bytes(n_rows, n_replicas);
+}
+
+namespace {
+
+int check_kv(const hx_kv_pool* p, const hx_kv_rows* r, const void* workspace, size_t workspace_bytes) {
+    if (!p || p->n_replicas < 1 || p->n_replicas > 255 || p->block_size < 1 || p->block_size > 65536) return HX_EINVAL;
+    if (!p->base || !p->free_list || !p->free_count || !p->free_out) return HX_EINVAL;
+    if (!r || r->n_rows < 1 || r->max_blocks < 1 || r->table_stride < r->max_blocks) return HX_EINVAL;
+    if (!r->block_table || !r->replica || !r->held || !r->held_out) return HX_EINVAL;
+    if (!workspace || ((uintptr_t)workspace & 255) ||
+        workspace_bytes < hx::kv_workspace_bytes(r->n_rows, p->n_replicas))
+        return HX_EINVAL;
+    return HX_OK;
+}
+
+}  // namespace
+
+int hx_kv_place(const hx_kv_pool* pool, const hx_kv_rows* rows, const int32_t* n_new, int64_t* tok_base,
+                int64_t* slots, int64_t max_slots, uint8_t* placed, void* workspace, size_t workspace_bytes,
+                hipStream_t stream) {
+    int rc = check_kv(pool, rows, workspace, workspace_bytes);
+    if (rc) return rc;
+    if (!n_new || !tok_base || !placed || max_slots < 0 || (max_slots > 0 && !slots)) return HX_EINVAL;
+    hipError_t e = hx::launch_place(*pool, *rows, n_new, tok_base, slots, max_slots, placed, workspace, stream);
+    return e == hipSuccess ? HX_OK : hip_error(e);
+}
+
+int hx_kv_release(const hx_kv_pool* pool, const hx_kv_rows* rows, const uint8_t* done, void* workspace,
+                  size_t workspace_bytes, hipStream_t stream) {
+    int rc = check_kv(pool, rows, workspace, workspace_bytes);
+    if (rc) return rc;
+    if (!done) return HX_EINVAL;
+    hipError_t e = hx::launch_release(*pool, *rows, done, workspace, stream);
     return e == hipSuccess ? HX_OK : hip_error(e);
 }
 

@@ -86,7 +86,7 @@ __device__ __forceinline__ int split_layers(const LayerSplit& s, int j, double c
 // Kernels of libhx, for the diagnostic per-kernel timing behind hx_profile.
 enum KernelId {
     kKSetup, kKDecode, kKScatter, kKEval, kKNodes, kKKv, kKMaxflow, kKBest, kKClasses, kKMoves, kKGather,
-    kKSpectral, kKPartition, kKShared, kKCount
+    kKSpectral, kKPartition, kKShared, kKSample, kKRoute, kKPlace, kKRelease, kKCount
 };
 // While profiling is enabled, records a HIP event on s before (end = false) or after
 // (end = true) a launch of kernel k; does nothing otherwise.
@@ -182,5 +182,29 @@ hipError_t launch_partition(const Problem& p, int64_t* w, const int32_t* order, 
                             uint8_t* role, hipStream_t s);
 hipError_t launch_gather(int32_t G, int32_t K, int32_t Ns, const uint8_t* sa, const uint8_t* sr, const int32_t* index,
                          int32_t count, uint8_t* da, uint8_t* dr, hipStream_t s);
+
+// Draws from scored rows (hx_sample): the call's arrays, with the parameters' pointers as given.
+struct SampleArgs {
+    int32_t R, N, type;
+    int64_t stride;
+    const void* data;
+    const float *temperature, *top_p, *min_p;
+    const int32_t* top_k;
+    const uint64_t* rnd;
+    int32_t *pick, *kept;
+    float* logp;
+};
+size_t sample_workspace_bytes(int32_t R, int32_t N);
+hipError_t launch_sample(const SampleArgs& a, void* workspace, hipStream_t s);
+
+// Dispatch: routes along a flow assignment, and the paged KV memory of the replicas.
+size_t route_workspace_bytes(int32_t max_p, int32_t max_d, int32_t max_pd, int32_t n_req);
+hipError_t launch_route(const FlowNet& f, int32_t cand, const int32_t* kv_flow, const uint64_t* rnd, const hx_routes& o,
+                        void* workspace, hipStream_t s);
+size_t kv_workspace_bytes(int32_t n_rows, int32_t n_replicas);
+hipError_t launch_place(const hx_kv_pool& p, const hx_kv_rows& r, const int32_t* n_new, int64_t* tok_base,
+                        int64_t* slots, int64_t max_slots, uint8_t* placed, void* workspace, hipStream_t s);
+hipError_t launch_release(const hx_kv_pool& p, const hx_kv_rows& r, const uint8_t* done, void* workspace,
+                          hipStream_t s);
 
 }  // namespace hx

@@ -9,6 +9,10 @@ the refinement calls of Sec. 3.4
 
     edge_classes, guided_moves, gather_candidates
 
+what a search or a coordinator does with scored placements
+
+    sample, route_requests, kv_place, kv_release
+
 and `DeviceProblem` uploads a seeded `inputs.Problem` once so that repeated calls read
 device-resident inputs.  There is no fallback: without the built library or a GPU every
 call raises.
@@ -96,13 +100,39 @@ class hx_flownet(C.Structure):
                 ("sink_cap", C.c_void_p)]
 
 
+class hx_scores(C.Structure):
+    _fields_ = [("n_rows", C.c_int32), ("n_cols", C.c_int32), ("type", C.c_int32), ("row_stride", C.c_int64),
+                ("data", C.c_void_p)]
+
+
+class hx_sampling(C.Structure):
+    _fields_ = [("temperature", C.c_void_p), ("top_k", C.c_void_p), ("top_p", C.c_void_p), ("min_p", C.c_void_p)]
+
+
+class hx_routes(C.Structure):
+    _fields_ = [("n_req", C.c_int32), ("prefill", C.c_void_p), ("decode", C.c_void_p), ("p_order", C.c_void_p),
+                ("p_base", C.c_void_p), ("d_order", C.c_void_p), ("d_base", C.c_void_p)]
+
+
+class hx_kv_pool(C.Structure):
+    _fields_ = [("n_replicas", C.c_int32), ("block_size", C.c_int32), ("base", C.c_void_p), ("free_list", C.c_void_p),
+                ("free_count", C.c_void_p), ("free_out", C.c_void_p)]
+
+
+class hx_kv_rows(C.Structure):
+    _fields_ = [("n_rows", C.c_int32), ("max_blocks", C.c_int32), ("table_stride", C.c_int64),
+                ("block_table", C.c_void_p), ("replica", C.c_void_p), ("held", C.c_void_p), ("held_out", C.c_void_p)]
+
+
 EXPORTS = ("hx_validate", "hx_cost_eval", "hx_cost_eval_static", "hx_static_scratch_bytes", "hx_cost_workspace_bytes", "hx_member_words", "hx_build_flownet",
            "hx_maxflow_batch", "hx_maxflow_stats", "hx_best_candidate", "hx_score_batch", "hx_score_workspace_bytes", "hx_edge_classes", "hx_guided_moves",
            "hx_gather_candidates",
            "hx_partition_workspace_bytes", "hx_spectral_order", "hx_partition_candidates",
+           "hx_sample_workspace_bytes", "hx_sample", "hx_route_workspace_bytes", "hx_route_requests",
+           "hx_kv_workspace_bytes", "hx_kv_place", "hx_kv_release",
            "hx_profile", "hx_profile_read", "hx_kernel_name", "hx_strerror", "hx_last_error",
            "hx_abi_version")
-HX_KERNELS = 14
+HX_KERNELS = 18
 
 _lib = None
 
@@ -147,6 +177,19 @@ def lib() -> C.CDLL:
                                         C.c_void_p]
         L.hx_partition_candidates.argtypes = [P(hx_cluster), hx_model, hx_workload, C.c_int32, C.c_void_p, C.c_size_t,
                                               C.c_void_p, C.c_int32, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p]
+        L.hx_sample_workspace_bytes.argtypes = [C.c_int32, C.c_int32]
+        L.hx_sample_workspace_bytes.restype = C.c_size_t
+        L.hx_sample.argtypes = [P(hx_scores), P(hx_sampling), C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p,
+                                C.c_void_p, C.c_size_t, C.c_void_p]
+        L.hx_route_workspace_bytes.argtypes = [C.c_int32, C.c_int32, C.c_int32, C.c_int32]
+        L.hx_route_workspace_bytes.restype = C.c_size_t
+        L.hx_route_requests.argtypes = [P(hx_flownet), C.c_int32, C.c_void_p, C.c_void_p, P(hx_routes), C.c_void_p,
+                                        C.c_size_t, C.c_void_p]
+        L.hx_kv_workspace_bytes.argtypes = [C.c_int32, C.c_int32]
+        L.hx_kv_workspace_bytes.restype = C.c_size_t
+        L.hx_kv_place.argtypes = [P(hx_kv_pool), P(hx_kv_rows), C.c_void_p, C.c_void_p, C.c_void_p, C.c_int64,
+                                  C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p]
+        L.hx_kv_release.argtypes = [P(hx_kv_pool), P(hx_kv_rows), C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p]
         L.hx_profile.argtypes = [C.c_int32]
         L.hx_profile.restype = C.c_int
         L.hx_profile_read.argtypes = [C.c_void_p, C.c_void_p, C.c_int32]
@@ -448,6 +491,228 @@ def score_batch(dp: DeviceProblem, ws: Workspace, stream=None) -> None:
     _check(lib().hx_score_batch(C.byref(dp.cluster), dp.model, dp.workload, dp.space, C.byref(dp.cand), C.byref(o),
                                 C.byref(f), _ptr(ws.flow_value), _ptr(ws.best), _ptr(ws.cost.workspace),
                                 C.c_size_t(int(ws.cost.workspace.numel())), _stream(stream)), "hx_score_batch")
+
+
+# ------------------------------------------------------------------ drawing from scored rows
+
+def _need(name: str, t, dtypes, shape=None, near=None):
+    """Refuses a tensor of another type, shape or device than the call reads or writes, or one with gaps."""
+    dtypes = dtypes if isinstance(dtypes, tuple) else (dtypes,)
+    if t.dtype not in dtypes:
+        raise ValueError(f"{name}: {t.dtype}, not {' or '.join(str(d) for d in dtypes)}")
+    if shape is not None and tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{name}: shape {tuple(t.shape)}, not {tuple(shape)}")
+    if not t.is_cuda or (near is not None and t.device != near):
+        raise ValueError(f"{name}: on {t.device}, not {'a GPU' if near is None else near}")
+    if shape is not None and not t.is_contiguous():
+        raise ValueError(f"{name}: not contiguous")
+
+
+def _own_stream(device, stream):
+    """The call's stream: the given one, or the device's current one; streams of another device are refused."""
+    torch = _torch()
+    s = torch.cuda.current_stream(device) if stream is None else stream
+    if s.device != device:
+        raise ValueError(f"a stream of {s.device} for tensors on {device}")
+    return C.c_void_p(int(s.cuda_stream))
+
+
+def _scratch(nbytes: int, device, what: str):
+    torch = _torch()
+    if nbytes <= 0:
+        raise ValueError(f"invalid sizes for the scratch of {what}")
+    return torch.empty(nbytes, dtype=torch.uint8, device=device)
+
+
+@dataclasses.dataclass
+class Sampling:
+    """Per-row parameters of `sample`, each a device tensor of one entry a row or None for off: temperature,
+    top_p and min_p float32, top_k int32."""
+    temperature: object = None
+    top_k: object = None
+    top_p: object = None
+    min_p: object = None
+
+
+@dataclasses.dataclass
+class SampleBuffers:
+    """Outputs of `sample` (int32, float32, int32, one entry a row; logp and kept may be None) and its scratch."""
+    pick: object
+    logp: object
+    kept: object
+    workspace: object
+
+    @classmethod
+    def empty(cls, n_rows: int, n_cols: int, device: str = "cuda") -> "SampleBuffers":
+        torch = _torch()
+        z = lambda dt: torch.empty(n_rows, dtype=dt, device=device)
+        return cls(z(torch.int32), z(torch.float32), z(torch.int32),
+                   _scratch(int(lib().hx_sample_workspace_bytes(n_rows, n_cols)), device, "sample"))
+
+
+def sample(scores, rnd, out: SampleBuffers, params: Optional[Sampling] = None, stream=None) -> SampleBuffers:
+    """One entry of every row of scores by temperature, top-k, top-p and min-p (hx_sample).  scores [rows, columns]:
+    int32 (flow values), float32, float16 or bfloat16; rows may overlap or repeat (a stride of 0), entries of a row
+    must be next to each other.  rnd: one 64-bit draw a row (int64 bit patterns)."""
+    torch = _torch()
+    types = {torch.int32: 0, torch.float32: 1, torch.float16: 2, torch.bfloat16: 3}
+    _need("scores", scores, tuple(types))
+    if scores.dim() != 2 or (scores.shape[1] > 1 and scores.stride(1) != 1):
+        raise ValueError("scores: two dimensions, the entries of a row next to each other")
+    R, dev = int(scores.shape[0]), scores.device
+    p = params if params is not None else Sampling()
+    _need("rnd", rnd, torch.int64, (R,), dev)
+    for name, t, dt in (("temperature", p.temperature, torch.float32), ("top_k", p.top_k, torch.int32),
+                        ("top_p", p.top_p, torch.float32), ("min_p", p.min_p, torch.float32),
+                        ("pick", out.pick, torch.int32), ("logp", out.logp, torch.float32),
+                        ("kept", out.kept, torch.int32)):
+        if t is not None:
+            _need(name, t, dt, (R,), dev)
+    _need("workspace", out.workspace, torch.uint8, (out.workspace.numel(),), dev)
+    sc = hx_scores(R, int(scores.shape[1]), types[scores.dtype], int(scores.stride(0)), _ptr(scores))
+    sp = hx_sampling(_ptr(p.temperature), _ptr(p.top_k), _ptr(p.top_p), _ptr(p.min_p))
+    with torch.cuda.device(dev):
+        _check(lib().hx_sample(C.byref(sc), C.byref(sp), _ptr(rnd), _ptr(out.pick), _ptr(out.logp), _ptr(out.kept),
+                               _ptr(out.workspace), C.c_size_t(int(out.workspace.numel())), _own_stream(dev, stream)),
+               "hx_sample")
+    return out
+
+
+# ------------------------------------------------------------------ dispatch (Sec. 3.3, 4)
+
+@dataclasses.dataclass
+class RouteBuffers:
+    """Outputs of `route_requests`, all int32 (the order and base of a side may both be None), and its scratch."""
+    dims: Tuple[int, int, int]
+    prefill: object
+    decode: object
+    p_order: object
+    p_base: object
+    d_order: object
+    d_base: object
+    workspace: object
+
+    @classmethod
+    def empty(cls, dims: Tuple[int, int, int], n_req: int, device: str = "cuda") -> "RouteBuffers":
+        torch = _torch()
+        mp, md, mpd = dims
+        z = lambda n: torch.empty(n, dtype=torch.int32, device=device)
+        return cls(tuple(dims), z(n_req), z(n_req), z(n_req), z(mp + 1), z(n_req), z(md + 1),
+                   _scratch(int(lib().hx_route_workspace_bytes(mp, md, mpd, n_req)), device, "route_requests"))
+
+
+def route_requests(net: FlowNetBuffers, kv_flow, rnd, out: RouteBuffers, cand: int = 0, stream=None) -> RouteBuffers:
+    """A KV edge for every request, drawn in proportion to the flows of column cand (hx_route_requests).
+    rnd: one 64-bit draw a request (int64 bit patterns)."""
+    torch = _torch()
+    mp, md, mpd = net.dims
+    n, dev, N = int(rnd.shape[0]), rnd.device, int(net.n_p.shape[0])
+    _need("rnd", rnd, torch.int64, (n,))
+    _need("kv_flow", kv_flow, torch.int32, (mpd, N), dev)
+    for name, t, shape in (("n_p", net.n_p, (N,)), ("n_d", net.n_d, (N,)), ("prefill", out.prefill, (n,)),
+                           ("decode", out.decode, (n,)), ("p_order", out.p_order, (n,)),
+                           ("p_base", out.p_base, (mp + 1,)), ("d_order", out.d_order, (n,)),
+                           ("d_base", out.d_base, (md + 1,))):
+        if t is not None:
+            _need(name, t, torch.int32, shape, dev)
+    _need("workspace", out.workspace, torch.uint8, (out.workspace.numel(),), dev)
+    f = net.struct()
+    o = hx_routes(n, _ptr(out.prefill), _ptr(out.decode), _ptr(out.p_order), _ptr(out.p_base), _ptr(out.d_order),
+                  _ptr(out.d_base))
+    with torch.cuda.device(dev):
+        _check(lib().hx_route_requests(C.byref(f), C.c_int32(cand), _ptr(kv_flow), _ptr(rnd), C.byref(o),
+                                       _ptr(out.workspace), C.c_size_t(int(out.workspace.numel())),
+                                       _own_stream(dev, stream)), "hx_route_requests")
+    return out
+
+
+@dataclasses.dataclass
+class KvPool:
+    """Paged KV memory of the replicas (hx_kv_pool): blocks of block_size tokens, base [replicas + 1], free_list and
+    free_count int32."""
+    block_size: int
+    base: object
+    free_list: object
+    free_count: object
+
+    @classmethod
+    def create(cls, blocks, block_size: int, device: str = "cuda") -> "KvPool":
+        """blocks[r] blocks for replica r, all free, its lowest block taken first."""
+        b = np.asarray(blocks, np.int64).reshape(-1)
+        if len(b) < 1 or b.min() < 0 or b.sum() > np.iinfo(np.int32).max:
+            raise ValueError("blocks: one count >= 0 a replica, fewer than 2^31 in all")
+        torch = _torch()
+        base = np.concatenate([[0], np.cumsum(b)])
+        lists = [np.arange(n - 1, -1, -1) for n in b] + ([] if b.sum() else [np.zeros(1)])  # never an empty tensor
+        dev = lambda a: torch.as_tensor(a.astype(np.int32)).to(device)
+        return cls(int(block_size), dev(base), dev(np.concatenate(lists)), dev(b))
+
+
+@dataclasses.dataclass
+class KvRows:
+    """Rows of a serving batch (hx_kv_rows): table [rows, blocks], replica and held [rows], all int32."""
+    table: object
+    replica: object
+    held: object
+
+    @classmethod
+    def empty(cls, n_rows: int, max_blocks: int, device: str = "cuda") -> "KvRows":
+        """Rows on no replica that hold nothing."""
+        torch = _torch()
+        z = lambda shape, v: torch.full(shape, v, dtype=torch.int32, device=device)
+        return cls(z((n_rows, max_blocks), -1), z((n_rows,), -1), z((n_rows,), 0))
+
+
+def kv_workspace(n_rows: int, n_replicas: int, device: str = "cuda"):
+    return _scratch(int(lib().hx_kv_workspace_bytes(n_rows, n_replicas)), device, "kv_place")
+
+
+def _kv_structs(pool: KvPool, rows: KvRows, workspace, free_out, held_out):
+    torch = _torch()
+    dev = rows.table.device
+    n, R = int(rows.replica.shape[0]), int(pool.free_count.shape[0])
+    free_out = pool.free_count if free_out is None else free_out
+    held_out = rows.held if held_out is None else held_out
+    _need("table", rows.table, torch.int32)
+    if rows.table.dim() != 2 or rows.table.shape[0] != n or (rows.table.shape[1] > 1 and rows.table.stride(1) != 1):
+        raise ValueError("table: one row a request, the entries of a row next to each other")
+    width, stride = int(rows.table.shape[1]), int(rows.table.stride(0)) if n > 1 else int(rows.table.shape[1])
+    for name, t, shape in (("replica", rows.replica, (n,)), ("held", rows.held, (n,)), ("held_out", held_out, (n,)),
+                           ("base", pool.base, (R + 1,)), ("free_list", pool.free_list, (pool.free_list.numel(),)),
+                           ("free_count", pool.free_count, (R,)), ("free_out", free_out, (R,))):
+        _need(name, t, torch.int32, shape, dev)
+    _need("workspace", workspace, torch.uint8, (workspace.numel(),), dev)
+    return (hx_kv_pool(R, int(pool.block_size), _ptr(pool.base), _ptr(pool.free_list), _ptr(pool.free_count),
+                       _ptr(free_out)),
+            hx_kv_rows(n, width, stride, _ptr(rows.table), _ptr(rows.replica), _ptr(rows.held), _ptr(held_out)), dev, n)
+
+
+def kv_place(pool: KvPool, rows: KvRows, n_new, tok_base, slots, placed, workspace, free_out=None, held_out=None,
+             stream=None) -> None:
+    """Blocks and token slots for n_new (int32) more tokens of every row (hx_kv_place): tok_base int64 [rows + 1],
+    slots int64, placed uint8 [rows].  The pool's free counts and the rows' lengths are updated in place unless
+    free_out / held_out are given."""
+    torch = _torch()
+    p, r, dev, n = _kv_structs(pool, rows, workspace, free_out, held_out)
+    _need("n_new", n_new, torch.int32, (n,), dev)
+    _need("tok_base", tok_base, torch.int64, (n + 1,), dev)
+    _need("slots", slots, torch.int64, (slots.numel(),), dev)
+    _need("placed", placed, torch.uint8, (n,), dev)
+    with torch.cuda.device(dev):
+        _check(lib().hx_kv_place(C.byref(p), C.byref(r), _ptr(n_new), _ptr(tok_base), _ptr(slots),
+                                 C.c_int64(int(slots.numel())), _ptr(placed), _ptr(workspace),
+                                 C.c_size_t(int(workspace.numel())), _own_stream(dev, stream)), "hx_kv_place")
+
+
+def kv_release(pool: KvPool, rows: KvRows, done, workspace, free_out=None, held_out=None, stream=None) -> None:
+    """The blocks of the rows with done (uint8) set back to their replicas (hx_kv_release); free counts and lengths as
+    for kv_place."""
+    torch = _torch()
+    p, r, dev, n = _kv_structs(pool, rows, workspace, free_out, held_out)
+    _need("done", done, torch.uint8, (n,), dev)
+    with torch.cuda.device(dev):
+        _check(lib().hx_kv_release(C.byref(p), C.byref(r), _ptr(done), _ptr(workspace),
+                                   C.c_size_t(int(workspace.numel())), _own_stream(dev, stream)), "hx_kv_release")
 
 
 # ------------------------------------------------------------------ refinement (Sec. 3.4)

@@ -1,0 +1,334 @@
+"""hx_sample on the GPU against the plain version in 64 bits (oracle/draws.py): picks and counts equal, log
+probabilities within float32's rounding.  A pick is a comparison of running sums whose terms agree to about
+2^-50, so that on these fixed seeds (no draw is within that of a border, or the weights are exact) it is the same."""
+import sys
+
+import numpy as np
+import pytest
+
+from oracle import draws as O
+from paper_2502_07903_amd import hx
+
+pytestmark = pytest.mark.gpu
+TYPES = ("i32", "f32", "f16", "bf16")
+
+
+def say(msg: str) -> None:
+    print(f"[gpu] {msg}", flush=True)
+    sys.stdout.flush()
+
+
+@pytest.fixture(scope="module")
+def torch():
+    import torch as T
+    if not T.cuda.is_available():
+        pytest.fail("GPU tests need a ROCm GPU (torch.cuda.is_available() is False)")
+    hx.lib()
+    return T
+
+
+def dtype(torch, name):
+    return {"i32": torch.int32, "f32": torch.float32, "f16": torch.float16, "bf16": torch.bfloat16}[name]
+
+
+def bits(rng, n):
+    return rng.integers(0, 1 << 64, n, dtype=np.uint64)
+
+
+def scores(rng, name, R, N, spread=1.0):
+    if name == "i32":
+        return rng.normal(9000, 1500 * spread, (R, N)).astype(np.int32)
+    return (rng.exponential(spread, (R, N)) - 3.0).astype(np.float32)
+
+
+def params(rng, R, which, i32=False):
+    out = dict(T=None, k=None, p=None, q=None)
+    out["T"] = (rng.uniform(150, 900, R) if i32 else rng.uniform(0.5, 1.5, R)).astype(np.float32)
+    if "k" in which:
+        out["k"] = rng.integers(0, 200, R).astype(np.int32)
+    if "p" in which:
+        out["p"] = rng.uniform(0.3, 1.02, R).astype(np.float32)
+    if "q" in which:
+        out["q"] = rng.uniform(-0.01, 0.2, R).astype(np.float32)
+    return out
+
+
+def device_params(torch, par):
+    dev = lambda a: None if a is None else torch.as_tensor(a).to("cuda")
+    return hx.Sampling(dev(par["T"]), dev(par["k"]), dev(par["p"]), dev(par["q"]))
+
+
+def device_draws(torch, draws):
+    return torch.as_tensor(np.asarray(draws, np.uint64).view(np.int64)).to("cuda")
+
+
+def compare(out, want, tag=""):
+    pick, logp, kept = (t.cpu().numpy() for t in (out.pick, out.logp, out.kept))
+    assert np.array_equal(kept, want[2]), f"{tag}: kept {kept[kept != want[2]][:5]}, not {want[2][kept != want[2]][:5]}"
+    assert np.array_equal(pick, want[0]), f"{tag}: picks differ in rows {np.flatnonzero(pick != want[0])[:5]}"
+    # float32's half step, and the 64-bit sum's own error
+    fin = np.isfinite(want[1])
+    assert np.array_equal(np.isneginf(logp), ~fin), tag
+    err = np.abs(logp[fin] - want[1][fin])
+    assert (err <= np.abs(want[1][fin]) * 2.0 ** -24 * 1.001 + 1e-11).all(), f"{tag}: logp off by {err.max()}"
+
+
+def check(torch, x_dev, draws, par, tag=""):
+    """One call, poisoned outputs, against the plain version on the same device values."""
+    R, N = x_dev.shape
+    out = hx.SampleBuffers.empty(R, N)
+    for t in (out.pick, out.kept, out.workspace):
+        t.fill_(0x55)
+    hx.sample(x_dev, device_draws(torch, draws), out, device_params(torch, par))
+    torch.cuda.synchronize()
+    host = x_dev.cpu()
+    host = host.numpy() if host.dtype in (torch.int32, torch.float32) else host.float().numpy()
+    compare(out, O.sample(host, draws, par["T"], par["k"], par["p"], par["q"]), tag)
+    return out
+
+
+@pytest.mark.parametrize("name", TYPES)
+@pytest.mark.parametrize("R,N", [(1, 1), (5, 2), (3, 63), (4, 64), (3, 65), (2, 1000), (7, 1023), (2, 1024), (3, 1025),
+                                 (2, 4097), (3, 8192), (2, 16385), (2, 32000), (3, 50257), (2, 65537), (1, 131072)])
+def test_sizes(torch, name, R, N):
+    rng = np.random.default_rng([11, R, N, TYPES.index(name)])
+    x = torch.as_tensor(scores(rng, name, R, N)).to("cuda").to(dtype(torch, name))
+    for which in ("", "k", "p", "q", "kp", "kpq"):
+        say(f"sample {name} {R} x {N} filters '{which}'")
+        check(torch, x, bits(rng, R), params(rng, R, which, name == "i32"), f"{name} {R}x{N} {which}")
+
+
+@pytest.mark.parametrize("name", TYPES)
+@pytest.mark.parametrize("R,N", [(300, 33), (40, 5000), (700, 3000), (257, 40000)])
+def test_many_rows(torch, name, R, N):
+    rng = np.random.default_rng([12, R, N, TYPES.index(name)])
+    say(f"sample {name} {R} x {N}")
+    spread = rng.choice([0.01, 0.3, 1.0, 3.0], (R, 1))  # from flat rows, which keep most entries, to peaked ones
+    x = torch.as_tensor(scores(rng, name, R, N, spread)).to("cuda").to(dtype(torch, name))
+    for which in ("", "p", "kpq"):
+        check(torch, x, bits(rng, R), params(rng, R, which, name == "i32"), f"{name} {R}x{N} {which}")
+
+
+@pytest.mark.parametrize("name", TYPES)
+@pytest.mark.parametrize("N", [37, 3000, 70000])
+def test_ties(torch, name, N):
+    """Three values only: the cuts of top-k and top-p fall inside runs of equal scores, which count by index."""
+    rng = np.random.default_rng([13, N, TYPES.index(name)])
+    R = 12
+    x = rng.choice([0.0, 1.0, 2.0], (R, N), p=[0.5, 0.3, 0.2])
+    x[1] = 7.0   # one value
+    x[2] = np.where(rng.random(N) < 0.5, 0.0, -0.0)
+    dev = torch.as_tensor(x.astype(np.float32)).to("cuda").to(dtype(torch, name))
+    k = rng.integers(1, N + 1, R).astype(np.int32)
+    k[3] = (x[3] == 2).sum()            # exactly the highest run
+    k[4] = (x[4] == 2).sum() + 1        # one of the next
+    p = rng.uniform(0.05, 0.99, R).astype(np.float32)
+    p[1], k[1] = 0.5, N                 # exact weights: half of the entries
+    T = np.full(R, 1.0, np.float32)
+    for par in (dict(T=T, k=k, p=None, q=None), dict(T=T, k=None, p=p, q=None), dict(T=T, k=k, p=p, q=None),
+                dict(T=T, k=None, p=None, q=np.full(R, 0.3, np.float32))):
+        say(f"sample ties {name} N={N}")
+        check(torch, dev, bits(rng, R), par, f"ties {name} {N}")
+
+
+@pytest.mark.parametrize("name", ("f32", "f16", "bf16"))
+def test_masks(torch, name):
+    dt = dtype(torch, name)
+    low, big = torch.finfo(dt).min, torch.finfo(dt).max
+    inf, nan = float("inf"), float("nan")
+    N = 2050
+    x = torch.randn((12, N), generator=torch.Generator().manual_seed(5))
+    x[0] = -inf
+    x[1] = nan
+    x[2] = torch.where(torch.arange(N) % 2 == 0, -inf, nan)
+    x[3] = low                      # a row masked with the type's lowest value keeps its entries
+    x[4, :] = low
+    x[4, 1500] = 1.0
+    x[5, 700] = inf
+    x[6, 700:703] = inf             # equal among the infinite ones
+    x[7, ::3] = nan
+    x[8, 1:] = -inf                 # one entry left
+    x[9, :] = -inf
+    x[9, N - 1] = low
+    x[10] = torch.where(torch.arange(N) % 2 == 0, big, low)
+    dev = x.to(dt).to("cuda")
+    rng = np.random.default_rng(14)
+    T = np.ones(12, np.float32)
+    for par in (dict(T=None, k=None, p=None, q=None), dict(T=T * 0, k=None, p=None, q=None),
+                dict(T=T, k=np.full(12, 5, np.int32), p=None, q=None),
+                dict(T=T * 1e30, k=None, p=T * 0.5, q=None), dict(T=T * 1e-40, k=None, p=T * 0.9, q=None),
+                dict(T=T, k=np.full(12, 9, np.int32), p=T * 0.7, q=T * 0.1)):
+        for draws in (bits(rng, 12), np.zeros(12, np.uint64), np.full(12, (1 << 64) - 1, np.uint64)):
+            say(f"sample masks {name}")
+            check(torch, dev, draws, par, f"masks {name}")
+
+
+def test_masked_int(torch):
+    rng = np.random.default_rng(15)
+    x = rng.integers(-(1 << 31), 1 << 31, (6, 3001)).astype(np.int32)
+    x[0] = O.I32_MIN
+    x[1] = O.I32_MIN
+    x[1, 17] = O.I32_MIN + 1
+    x[2] = (1 << 31) - 1
+    x[3, ::2] = O.I32_MIN
+    dev = torch.as_tensor(x).to("cuda")
+    T = np.full(6, 3e8, np.float32)
+    for par in (dict(T=None, k=None, p=None, q=None), dict(T=T, k=None, p=None, q=None),
+                dict(T=T, k=np.full(6, 77, np.int32), p=np.full(6, 0.8, np.float32), q=None),
+                dict(T=T, k=None, p=np.full(6, 0.8, np.float32), q=np.full(6, 0.01, np.float32))):
+        say("sample masked int32")
+        check(torch, dev, bits(rng, 6), par, "masked int32")
+
+
+@pytest.mark.parametrize("N", [50, 9000])
+def test_parameters(torch, N):
+    """Every parameter at its edges; rows whose parameters are out of range draw nothing."""
+    inf, nan = np.inf, np.nan
+    T = [0, -0.0, 1e-45, 1e-3, 1, 1e38, inf, nan, -1, -inf]
+    k = [-5, 0, 1, 2, N - 1, N, N + 1, (1 << 31) - 1]
+    p = [-1, 0, 1e-30, 0.5, 0.999999, 1, 2, nan, inf, -inf]
+    q = [-1, 0, 1e-300, 1e-30, 0.5, 1, 1.0001, nan, inf, -inf]
+    rows = [(t, 0, 1, 0) for t in T] + [(1, a, 1, 0) for a in k] + [(1, 0, a, 0) for a in p] + [(1, 0, 1, a) for a in q]
+    R = len(rows)
+    rng = np.random.default_rng([16, N])
+    x = torch.as_tensor(scores(rng, "f32", R, N)).to("cuda")
+    f = lambda i: np.array([r[i] for r in rows]).astype(np.float32)
+    par = dict(T=f(0), k=np.array([r[1] for r in rows], np.int64).astype(np.int32), p=f(2), q=f(3))
+    say(f"sample parameters N={N}")
+    check(torch, x, bits(rng, R), par, "parameters")
+
+
+@pytest.mark.parametrize("name", TYPES)
+def test_strides(torch, name):
+    """Padded rows, rows that start off a vector's alignment, one row read by all, overlapping rows; what lies between
+    the rows is not read as a score."""
+    rng = np.random.default_rng([17, TYPES.index(name)])
+    dt = dtype(torch, name)
+    R, N = 9, 5003
+    big = torch.as_tensor(scores(rng, name, R, N + 13)).to("cuda").to(dt)
+    big[:, N + 1:] = 30000  # larger than every score
+    par = params(rng, R, "kp", name == "i32")
+    for tag, x in (("padded", big[:, :N]), ("offset", big[:, 1:N + 1]), ("shared", big[:1, :N].expand(R, N)),
+                   ("overlapping", big.view(-1)[:N + 9 * R].as_strided((R, N), (1, 1)))):
+        say(f"sample strides {name} {tag}")
+        check(torch, x, bits(rng, R), par, f"{tag} {name}")
+        check(torch, x, bits(rng, R), params(rng, R, "", name == "i32"), f"{tag} {name}")
+
+
+def test_offsets_past_32_bits(torch):
+    """Rows that start past 2^31 elements and 2^32 bytes."""
+    stride, R, N = (1 << 30) + 8, 4, 3001
+    say("sample rows 2^30 apart")
+    flat = torch.empty(stride * (R - 1) + N, dtype=torch.bfloat16, device="cuda")
+    x = flat.as_strided((R, N), (stride, 1))
+    rng = np.random.default_rng(18)
+    x.copy_(torch.as_tensor(scores(rng, "bf16", R, N)).to("cuda"))
+    check(torch, x, bits(rng, R), params(rng, R, "kp"), "far rows")
+
+
+@pytest.mark.parametrize("N", [(1 << 21) + 3, 262144])
+def test_long_row(torch, N):
+    rng = np.random.default_rng([19, N])
+    for name in ("i32", "bf16"):
+        x = torch.as_tensor(scores(rng, name, 2, N)).to("cuda").to(dtype(torch, name))
+        for which in ("", "kp"):
+            say(f"sample long row {name} {N} '{which}'")
+            check(torch, x, bits(rng, 2), params(rng, 2, which, name == "i32"), f"long {name}")
+
+
+def test_follows_the_weights(torch):
+    """The draws of one row with its probabilities: 40,000 draws of the same scores, frequencies within five standard
+    deviations of the kept probabilities."""
+    n = 40000
+    x = torch.log(torch.tensor([[1.0, 2.0, 3.0, 4.0, 0.5]])).to("cuda").expand(n, 5)
+    rng = np.random.default_rng(20)
+    out = hx.SampleBuffers.empty(n, 5)
+    k4 = torch.full((n,), 4, dtype=torch.int32, device="cuda")
+    say("sample frequencies")
+    hx.sample(x, device_draws(torch, bits(rng, n)), out, hx.Sampling(top_k=k4))
+    got = np.bincount(out.pick.cpu().numpy(), minlength=5) / n
+    want = np.array([0.1, 0.2, 0.3, 0.4, 0.0])
+    assert got[4] == 0 and (np.abs(got - want) <= 5 * np.sqrt(want * (1 - want) / n)).all()
+
+
+@pytest.mark.parametrize("R,N", [(2, 100), (3, 60000), (600, 1000)])
+def test_captured_and_replayed(torch, R, N):
+    """A captured call replayed on new scores and draws, with eager calls between the replays: each equal to the eager
+    call's outputs on the same inputs."""
+    rng = np.random.default_rng([21, R, N])
+    x = torch.zeros((R, N), device="cuda")
+    d = torch.zeros(R, dtype=torch.int64, device="cuda")
+    par = device_params(torch, params(rng, R, "kpq"))
+    out, eager = hx.SampleBuffers.empty(R, N), hx.SampleBuffers.empty(R, N)
+    say(f"sample captured {R} x {N}")
+    s = torch.cuda.Stream()
+    with torch.cuda.stream(s):
+        hx.sample(x, d, out, par)
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        hx.sample(x, d, out, par)
+    for i in range(4):
+        x.copy_(torch.as_tensor(scores(rng, "f32", R, N)))
+        d.copy_(device_draws(torch, bits(rng, R)))
+        g.replay()
+        hx.sample(x, d, eager, par)
+        torch.cuda.synchronize()
+        for a, b in ((out.pick, eager.pick), (out.kept, eager.kept), (out.logp, eager.logp)):
+            assert torch.equal(a, b), f"replay {i}"
+
+
+def test_two_streams_and_repeats(torch):
+    """Calls on two streams at once, each with buffers of its own, and the same call again: the same outputs, the
+    inputs unchanged."""
+    rng = np.random.default_rng(22)
+    R, N = 20, 30000
+    x = [torch.as_tensor(scores(rng, "f32", R, N)).to("cuda") for _ in range(2)]
+    d = [device_draws(torch, bits(rng, R)) for _ in range(2)]
+    par = device_params(torch, params(rng, R, "kp"))
+    before = [t.clone() for t in x]
+    alone = [hx.sample(x[i], d[i], hx.SampleBuffers.empty(R, N), par) for i in range(2)]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    outs = [hx.SampleBuffers.empty(R, N) for _ in range(2)]
+    torch.cuda.synchronize()
+    say("sample on two streams")
+    for _ in range(10):
+        for i in range(2):
+            hx.sample(x[i], d[i], outs[i], par, stream=streams[i])
+    torch.cuda.synchronize()
+    for i in range(2):
+        assert torch.equal(x[i], before[i])
+        for k in ("pick", "logp", "kept"):
+            assert torch.equal(getattr(outs[i], k), getattr(alone[i], k))
+
+
+def test_outputs_left_out(torch):
+    rng = np.random.default_rng(23)
+    x = torch.as_tensor(scores(rng, "f32", 3, 500)).to("cuda")
+    d = device_draws(torch, bits(rng, 3))
+    full = hx.sample(x, d, hx.SampleBuffers.empty(3, 500))
+    bare = hx.SampleBuffers.empty(3, 500)
+    bare.logp = bare.kept = None
+    hx.sample(x, d, bare)
+    assert torch.equal(full.pick, bare.pick)
+
+
+def test_refuses(torch):
+    x = torch.zeros((4, 50), device="cuda")
+    d = torch.zeros(4, dtype=torch.int64, device="cuda")
+    out = hx.SampleBuffers.empty(4, 50)
+    bad = [lambda: hx.sample(x.double(), d, out), lambda: hx.sample(x[0], d, out), lambda: hx.sample(x.t(), d, out),
+           lambda: hx.sample(x[:, ::2], d, out), lambda: hx.sample(x, d[:3], out), lambda: hx.sample(x, d.int(), out),
+           lambda: hx.sample(x, d.cpu(), out), lambda: hx.sample(x.cpu(), d, out), lambda: hx.sample(x[:3], d[:3], out),
+           lambda: hx.sample(x, d, out, hx.Sampling(top_k=torch.zeros(4, device="cuda"))),
+           lambda: hx.sample(x, d, out, hx.Sampling(temperature=torch.zeros(8, device="cuda")[::2])),
+           lambda: hx.sample(x, d, out, hx.Sampling(top_p=torch.zeros(5, device="cuda")))]
+    for f in bad:
+        with pytest.raises(ValueError):
+            f()
+    with pytest.raises(hx.HxError):
+        hx.sample(x[:0], d[:0], hx.SampleBuffers(out.pick[:0], out.logp[:0], out.kept[:0], out.workspace))
+    out.workspace = out.workspace[:0]
+    with pytest.raises(hx.HxError):
+        hx.sample(x, d, out)
