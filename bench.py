@@ -14,6 +14,10 @@ workload with per-GPU flow nodes): each round scores the parent placement with a
 assignment, classifies its edges, emits the children by guided moves, scores them and keeps
 the best; value = children per second.
 
+--dispatch times serving steps of the best placement of a scored batch instead: --requests requests
+routed along its maximum flow, their prompts' KV blocks and token slots, and eight steps of one
+token each; value = requests per second.
+
 Prints ONE JSON line.  Per-call durations come from HIP events recorded around every call
 inside the timed region, on the stream the kernels run on; per-kernel durations from a second
 pass of the same steps with libhx's diagnostic per-kernel events (hx_profile).  The roofline
@@ -121,6 +125,9 @@ def parse():
     ap.add_argument("--pushrelabel", choices=["workload3", "workload5"], default=None,
                     help="time the max-flow alone on networks that need push-relabel, at the network shapes of "
                          "that workload (both sides of at least two nodes, KV arcs below min(a_i, b_j))")
+    ap.add_argument("--dispatch", action="store_true",
+                    help="time requests routed over the best placement's maximum flow and given KV memory instead")
+    ap.add_argument("--requests", type=int, default=4096, help="requests per step (--dispatch)")
     ap.add_argument("--children", type=int, default=131072, help="children per refinement round (--refine)")
     ap.add_argument("--partition-candidates", type=int, default=16384, help="candidates per step (--partition)")
     ap.add_argument("--spectral-iters", type=int, default=1000, help="power iterations (--partition)")
@@ -651,6 +658,58 @@ def partition_main(args, torch, hx, I):
     print(json.dumps(out))
 
 
+def dispatch_main(args, torch, hx, I):
+    """The best placement of the workload's batch put to work: a step routes --requests requests along
+    its maximum flow, places their prompts in the decode replicas' KV blocks, places eight single
+    tokens for every request served, and gives the blocks back."""
+    cfg = args.workload
+    wl = I.WORKLOADS[cfg]
+    prob = I.make_problem(cfg, n_cand=args.candidates or None)
+    dp = hx.DeviceProblem.upload(prob)
+    ws = hx.Workspace.for_problem(dp)
+    hx.score_batch(dp, ws)
+    best = [int(x) for x in ws.best.cpu().numpy()]
+    n, tokens = args.requests, 8
+    lens = np.resize(I.request_lengths(wl)[0], n).astype(np.int32)
+    prompt = torch.as_tensor(lens).to("cuda")
+    rnd = torch.as_tensor(I.move_draws(cfg, 0, n).view(np.int64)).to("cuda")
+    d = hx.Dispatcher.create(dp, best[0], n, int(lens.max()) + tokens, int(lens.sum()))
+
+    def step():
+        d.admit(rnd, prompt)
+        for _ in range(tokens):
+            d.step()
+
+    for _ in range(args.warmup):
+        step()
+    torch.cuda.synchronize()
+    t0 = time.perf_counter()
+    for _ in range(args.steps):
+        step()
+    torch.cuda.synchronize()
+    ms = (time.perf_counter() - t0) * 1000.0 / args.steps
+    hx.profile(True)
+    for _ in range(args.steps):
+        step()
+    torch.cuda.synchronize()
+    prof = hx.profile_read()
+    hx.profile(False)
+    held = int((d.rows.held > 0).sum())
+    print(json.dumps({
+        "metric": "requests routed and given KV memory/sec (Sec. 3.3 flow, Sec. 4 paged memory) at 1 GPU",
+        "value": n / (ms / 1000.0),
+        "unit": "requests/s",
+        "n_gpus": 1, "steps": args.steps, "warmup": args.warmup, "ms_per_step": ms, "higher_is_better": True,
+        "scaling": "weak", "vs_baseline": None, "dtype": "i32+i64", "data": "synthetic",
+        "config": {"workload": f"workload{wl.cfg}: {wl.name}, its best placement", "requests": n,
+                   "prompt_tokens": int(lens.sum()), "decode_steps": tokens,
+                   "decode_replicas": int(d.ws.net.n_d[0]), "kv_blocks": int(d.pool.base[-1])},
+        "best": best,
+        "requests_served": held,
+        "kernel_us": {k: 1000.0 * v / c for k, (v, c) in prof.items() if c > 0},
+    }))
+
+
 def chain_main(args, torch, hx, I):
     """Workload 5 as defined: rounds of 131,072 single-step perturbations (45% move one GPU, 45%
     swap two GPUs, 10% merge two groups) of the previous round's best placement, the GPU argmax,
@@ -905,6 +964,9 @@ def main():
         return
     if args.partition:
         partition_main(args, torch, hx, I)
+        return
+    if args.dispatch:
+        dispatch_main(args, torch, hx, I)
         return
     if args.workload == 5:
         chain_main(args, torch, hx, I)

@@ -715,6 +715,79 @@ def kv_release(pool: KvPool, rows: KvRows, done, workspace, free_out=None, held_
                                    C.c_size_t(int(workspace.numel())), _own_stream(dev, stream)), "hx_kv_release")
 
 
+@dataclasses.dataclass
+class Dispatcher:
+    """Requests of one placement and the KV memory they take (Sec. 3.3, 4): the placement's maximum
+    flow routes every request to a prefill and a decode replica, and the decode replica's KV blocks
+    hold its tokens.  A decode replica has the blocks of the bmax requests of mean length
+    (s_in + s_out) that Table 1's memory limit admits.  Replica j of `pool` is decode node j of
+    `ws.net`; row i of `rows` is request i.  After `create` (which reads the placement's replicas
+    back once) no call synchronises."""
+    placement: DeviceProblem
+    ws: Workspace
+    routes: RouteBuffers
+    pool: KvPool
+    rows: KvRows
+    tok_base: object    # int64 [rows + 1], slots int64 and placed uint8 [rows]: of the last call
+    slots: object
+    placed: object
+    workspace: object
+    one: object         # int32 [rows], uint8 [rows]: scratch and constants of the calls below
+    all_rows: object
+
+    @classmethod
+    def create(cls, dp: DeviceProblem, cand: int, n_rows: int, max_tokens: int, max_slots: int, block_size: int = 16,
+               device: str = "cuda", stream=None) -> "Dispatcher":
+        """For column cand of dp (replica networks: granularity 0), n_rows requests of at most max_tokens tokens
+        each, and at most max_slots new tokens in one call."""
+        torch = _torch()
+        if dp.space.granularity != 0:
+            raise ValueError("requests are dispatched to replicas: granularity 0")
+        if n_rows < 1 or max_tokens < 1 or max_slots < 1 or block_size < 1:
+            raise ValueError("rows, tokens, slots and the block size must be at least 1")
+        one = dp.with_candidates(dp.tensors["assign"][:, cand:cand + 1].clone(),
+                                 dp.tensors["role"][:, cand:cand + 1].clone())
+        ws = Workspace.for_problem(one, flows=True, device=device)
+        score(one, ws, stream)
+        (torch.cuda.current_stream() if stream is None else stream).synchronize()
+        n_d = int(ws.net.n_d[0])
+        width = -(-max_tokens // block_size)
+        mean = -(-int(np.ceil(dp.workload.s_in + dp.workload.s_out)) // block_size)
+        bmax = ws.cost.bmax[:, 0].cpu().numpy().astype(np.int64)
+        blocks = np.zeros(ws.net.dims[1], np.int64)
+        blocks[:n_d] = np.minimum(bmax[ws.net.d_slot[:n_d, 0].cpu().numpy()] * mean, n_rows * width)
+        z = lambda n, dt, v=0: torch.full((n,), v, dtype=dt, device=device)
+        routes = RouteBuffers.empty(ws.net.dims, n_rows, device)
+        rows = KvRows.empty(n_rows, width, device)
+        rows.replica = routes.decode
+        rows.replica.fill_(-1)
+        return cls(one, ws, routes, KvPool.create(blocks, block_size, device), rows, z(n_rows + 1, torch.int64),
+                   z(max_slots, torch.int64), z(n_rows, torch.uint8), kv_workspace(n_rows, len(blocks), device),
+                   z(n_rows, torch.int32, 1), z(n_rows, torch.uint8, 1))
+
+    def admit(self, rnd, prompt, stream=None) -> None:
+        """A request in every row, over whatever the rows held: routed by its draw (rnd, int64 bit patterns), its
+        prompt's tokens (int32) placed.  Requests that were not (placed 0) keep their route and hold nothing."""
+        self.finish(self.all_rows, stream)
+        route_requests(self.ws.net, self.ws.kv_flow, rnd, self.routes, 0, stream)
+        self._place(prompt, stream)
+
+    def step(self, n_new=None, stream=None) -> None:
+        """n_new (int32) more tokens a row; by default one for every row that holds any (a decode step)."""
+        if n_new is None:
+            torch = _torch()
+            with torch.cuda.stream(stream):
+                n_new = torch.sign(self.rows.held, out=self.one)
+        self._place(n_new, stream)
+
+    def finish(self, done, stream=None) -> None:
+        """The blocks of the rows with done (uint8) set go back to their replicas."""
+        kv_release(self.pool, self.rows, done, self.workspace, stream=stream)
+
+    def _place(self, n_new, stream) -> None:
+        kv_place(self.pool, self.rows, n_new, self.tok_base, self.slots, self.placed, self.workspace, stream=stream)
+
+
 # ------------------------------------------------------------------ refinement (Sec. 3.4)
 
 def edge_classes(net: FlowNetBuffers, flow_value, kv_flow, node_cls, kv_cls, stream=None):
@@ -754,7 +827,12 @@ class Refiner:
       3. the children scored (value only) and the best chosen (lowest index on ties);
       4. the best child gathered into the parent for the next round.
     best_value after a round is the parent's new score; a round whose best index is 0 found
-    no improvement."""
+    no improvement.
+
+    A round given one 64-bit draw (`draw`, int64 of one entry) takes over a child drawn from the
+    children's flow values by `sampling` (hx_sample; temperature in milli-requests/s) instead of
+    the best: a chain that may pass through worse placements, and so leave a local maximum.
+    `drawn` then holds the child taken; best still names the best child."""
     parent: DeviceProblem
     parent_ws: Workspace
     node_cls: object
@@ -762,6 +840,7 @@ class Refiner:
     children: DeviceProblem
     child_ws: Workspace
     move: object
+    drawn: Optional[SampleBuffers] = None
 
     @classmethod
     def create(cls, dp: DeviceProblem, parent_col: int, n_child: int, device: str = "cuda",
@@ -779,15 +858,19 @@ class Refiner:
         return cls(parent, pws, torch.zeros((mp + md, 1), dtype=torch.uint8, device=device),
                    torch.zeros((mpd, 1), dtype=torch.uint8, device=device), children,
                    Workspace.for_problem(children, device=device),
-                   torch.empty(n_child, dtype=torch.int32, device=device))
+                   torch.empty(n_child, dtype=torch.int32, device=device),
+                   SampleBuffers.empty(1, n_child, device))
 
-    def round(self, rnd, stream=None) -> None:
+    def round(self, rnd, stream=None, draw=None, sampling: Optional[Sampling] = None) -> None:
         p, pw, ch, cw = self.parent, self.parent_ws, self.children, self.child_ws
         score(p, pw, stream)
         edge_classes(pw.net, pw.flow_value, pw.kv_flow, self.node_cls, self.kv_cls, stream)
         guided_moves(p, pw.net, self.node_cls, rnd, ch.tensors["assign"], ch.tensors["role"], self.move, stream)
         score_batch(ch, cw, stream)
-        gather_candidates(ch, cw.best[:1], p.tensors["assign"], p.tensors["role"], stream)
+        index = cw.best[:1]
+        if draw is not None:
+            index = sample(cw.flow_value.view(1, -1), draw, self.drawn, sampling, stream).pick
+        gather_candidates(ch, index, p.tensors["assign"], p.tensors["role"], stream)
 
 
 # ------------------------------------------------------------------ graph partition (Sec. 3.2)

@@ -1,0 +1,134 @@
+"""The draw and dispatch calls together, as a search and a coordinator make them: a batch scored, a placement drawn
+from it, refinement rounds whose parents are drawn, and the placement's requests routed, placed, stepped and released.
+Every stage is checked against the plain versions (oracle/draws.py) on what the stage before left on the device."""
+import sys
+
+import numpy as np
+import pytest
+
+from oracle import draws as O
+from oracle import hxo
+from paper_2502_07903_amd import hx
+from paper_2502_07903_amd import inputs as I
+
+pytestmark = pytest.mark.gpu
+
+
+def say(msg: str) -> None:
+    print(f"[gpu] {msg}", flush=True)
+    sys.stdout.flush()
+
+
+@pytest.fixture(scope="module")
+def torch():
+    import torch as T
+    if not T.cuda.is_available():
+        pytest.fail("GPU tests need a ROCm GPU (torch.cuda.is_available() is False)")
+    hx.lib()
+    return T
+
+
+def draws_of(torch, rng, n):
+    d = rng.integers(0, 1 << 64, n, dtype=np.uint64)
+    return d, torch.as_tensor(d.view(np.int64)).to("cuda")
+
+
+@pytest.mark.parametrize("cfg,n", [(1, 300), (5, 700)])
+def test_refiner_takes_the_drawn_child(torch, cfg, n):
+    """Rounds with draws: the next parent is the child that the plain draw picks from the children's flow values; a
+    round without a draw still takes the best."""
+    rng = np.random.default_rng([51, cfg])
+    prob = I.make_problem(cfg, n_cand=8)
+    dp = hx.DeviceProblem.upload(prob)
+    ref = hx.Refiner.create(dp, 3, n)
+    T = np.array([200.0], np.float32)
+    k = np.array([40], np.int32)
+    par = hx.Sampling(temperature=torch.as_tensor(T).to("cuda"), top_k=torch.as_tensor(k).to("cuda"))
+    for rnd in range(5):
+        say(f"refiner with draws: workload {cfg}, round {rnd}")
+        moves = torch.as_tensor(I.move_draws(cfg, rnd, n).view(np.int64)).to("cuda")
+        d, d_dev = draws_of(torch, rng, 1)
+        if rnd == 3:
+            ref.round(moves)
+            pick = int(ref.child_ws.best[0])
+        else:
+            ref.round(moves, draw=d_dev, sampling=par)
+            pick = O.sample(ref.child_ws.flow_value.cpu().numpy()[None], d, T, k)[0][0]
+            assert int(ref.drawn.pick[0]) == pick
+        torch.cuda.synchronize()
+        assert torch.equal(ref.parent.tensors["assign"][:, 0], ref.children.tensors["assign"][:, pick])
+        assert torch.equal(ref.parent.tensors["role"][:, 0], ref.children.tensors["role"][:, pick])
+
+
+@pytest.mark.parametrize("cfg,n_rows,bs", [(1, 60, 16), (2, 700, 8), (3, 2100, 16)])
+def test_from_scores_to_slots(torch, cfg, n_rows, bs):
+    rng = np.random.default_rng([52, cfg])
+    prob = I.make_problem(cfg, n_cand=512)
+    dp = hx.DeviceProblem.upload(prob)
+    ws = hx.Workspace.for_problem(dp)
+    hx.score_batch(dp, ws)
+    d, d_dev = draws_of(torch, rng, 1)
+    T, p = np.array([500.0], np.float32), np.array([0.9], np.float32)
+    out = hx.sample(ws.flow_value.view(1, -1), d_dev, hx.SampleBuffers.empty(1, 512),
+                    hx.Sampling(temperature=torch.as_tensor(T).to("cuda"), top_p=torch.as_tensor(p).to("cuda")))
+    value = hxo.score_batch(prob)["flow_value"]
+    cand = int(out.pick[0])
+    assert cand == O.sample(value[None], d, T, None, p)[0][0]
+
+    lens = np.clip(np.rint(rng.lognormal(5, 1, n_rows)), 1, 3000).astype(np.int32)
+    disp = hx.Dispatcher.create(dp, cand, n_rows, 3000 + 8, int(lens.sum()) + n_rows, block_size=bs)
+    assert int(disp.ws.flow_value[0]) == value[cand] and int(disp.ws.kv_flow.sum()) == value[cand]
+    n_p, n_d = int(disp.ws.net.n_p[0]), int(disp.ws.net.n_d[0])
+    pool = {k: getattr(disp.pool, k).cpu().numpy() for k in ("base", "free_list", "free_count")}
+    bmax = disp.ws.cost.bmax[:, 0].cpu().numpy()[disp.ws.net.d_slot[:n_d, 0].cpu().numpy()]
+    assert (np.diff(pool["base"])[:n_d] > 0).tolist() == (bmax > 0).tolist()
+    width = disp.rows.table.shape[1]
+    table = np.full((n_rows, width), -1, np.int32)
+    free, free_list = pool["free_count"].copy(), pool["free_list"].copy()
+    held = np.zeros(n_rows, np.int32)
+    for batch in range(2):
+        d, d_dev = draws_of(torch, rng, n_rows)
+        say(f"scores to slots: workload {cfg}, batch {batch}")
+        held, free = O.release(bs, pool["base"], free_list, free, table, width,
+                               disp.rows.replica.cpu().numpy(), held, np.ones(n_rows))
+        disp.admit(d_dev, torch.as_tensor(lens).to("cuda"))
+        want = O.route(n_p, n_d, *disp.ws.net.dims, disp.ws.kv_flow[:, 0].cpu().numpy(), d)
+        for k, v in want.items():
+            assert np.array_equal(getattr(disp.routes, k).cpu().numpy(), v), k
+        news = [lens, None, None]
+        for step, new in enumerate(news):
+            if step:
+                disp.step()
+            slots = disp.slots.cpu().numpy()
+            before = slots.copy()
+            new = (held > 0).astype(np.int32) if new is None else new
+            tok, placed, held, free = O.place(bs, pool["base"], free_list, free, table, width, want["decode"], held, new,
+                                              slots)
+            assert np.array_equal(before[:tok[-1]], slots[:tok[-1]])
+            assert np.array_equal(disp.placed.cpu().numpy(), placed)
+            assert np.array_equal(disp.tok_base.cpu().numpy(), tok)
+            assert np.array_equal(disp.rows.held.cpu().numpy(), held)
+            assert np.array_equal(disp.rows.table.cpu().numpy(), table)
+            assert np.array_equal(disp.pool.free_count.cpu().numpy(), free)
+        # no two tokens of a replica share a slot
+        rep = np.repeat(want["decode"], held * (held > 0))
+        blocks = [table[i, :-(-held[i] // bs)] for i in range(n_rows)]
+        for r in range(n_d):
+            mine = np.concatenate([blocks[i] for i in range(n_rows) if want["decode"][i] == r] + [np.zeros(0, np.int32)])
+            assert len(mine) == len(set(mine.tolist()))
+        assert rep.size == held.sum()
+        done = (rng.random(n_rows) < 0.5).astype(np.uint8)
+        disp.finish(torch.as_tensor(done).to("cuda"))
+        held, free = O.release(bs, pool["base"], free_list, free, table, width, want["decode"], held, done)
+        assert np.array_equal(disp.pool.free_list.cpu().numpy(), free_list)
+        assert np.array_equal(disp.pool.free_count.cpu().numpy(), free)
+
+
+def test_dispatcher_refuses(torch):
+    dp = hx.DeviceProblem.upload(I.make_problem(5, n_cand=2))
+    with pytest.raises(ValueError):
+        hx.Dispatcher.create(dp, 0, 8, 100, 100)
+    dp = hx.DeviceProblem.upload(I.make_problem(1, n_cand=2))
+    for bad in ((0, 100, 100, 16), (8, 0, 100, 16), (8, 100, 0, 16), (8, 100, 100, 0)):
+        with pytest.raises(ValueError):
+            hx.Dispatcher.create(dp, 0, *bad)
