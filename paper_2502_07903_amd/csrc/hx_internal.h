@@ -193,6 +193,7 @@ struct SampleArgs {
     const uint64_t* rnd;
     int32_t *pick, *kept;
     float* logp;
+    int64_t row0 = 0;  // first row of a launch
 };
 size_t sample_workspace_bytes(int32_t R, int32_t N);
 hipError_t launch_sample(const SampleArgs& a, void* workspace, hipStream_t s);

@@ -495,26 +495,38 @@ def score_batch(dp: DeviceProblem, ws: Workspace, stream=None) -> None:
 
 # ------------------------------------------------------------------ drawing from scored rows
 
-def _need(name: str, t, dtypes, shape=None, near=None):
-    """Refuses a tensor of another type, shape or device than the call reads or writes, or one with gaps."""
-    dtypes = dtypes if isinstance(dtypes, tuple) else (dtypes,)
-    if t.dtype not in dtypes:
-        raise ValueError(f"{name}: {t.dtype}, not {' or '.join(str(d) for d in dtypes)}")
-    if shape is not None and tuple(t.shape) != tuple(shape):
-        raise ValueError(f"{name}: shape {tuple(t.shape)}, not {tuple(shape)}")
-    if not t.is_cuda or (near is not None and t.device != near):
-        raise ValueError(f"{name}: on {t.device}, not {'a GPU' if near is None else near}")
-    if shape is not None and not t.is_contiguous():
-        raise ValueError(f"{name}: not contiguous")
+def _need(name: str, t, dtype, shape, index: int) -> None:
+    """Refuses a tensor of another type, shape or device than the call reads or writes, or one with gaps.  (One
+    condition, since a small call's time is mostly such checks: 0.3 us a tensor.)"""
+    if t.dtype is dtype and t.shape == shape and t.get_device() == index and t.is_contiguous():
+        return
+    raise ValueError(f"{name}: {t.dtype} {tuple(t.shape)} on {t.device}{'' if t.is_contiguous() else ', with gaps'}, "
+                     f"not {dtype} {tuple(shape)} on cuda:{index}")
 
 
-def _own_stream(device, stream):
-    """The call's stream: the given one, or the device's current one; streams of another device are refused."""
-    torch = _torch()
-    s = torch.cuda.current_stream(device) if stream is None else stream
-    if s.device != device:
-        raise ValueError(f"a stream of {s.device} for tensors on {device}")
-    return C.c_void_p(int(s.cuda_stream))
+def _gpu_of(name: str, t) -> int:
+    index = t.get_device()
+    if index < 0:
+        raise ValueError(f"{name}: on {t.device}, not a GPU")
+    return index
+
+
+def _launch(index: int, stream, where: str, fn, *args) -> None:
+    """fn(*args, stream) with the tensors' GPU current, on the given stream (one of another GPU is refused) or that
+    GPU's current one."""
+    import torch
+    if stream is None:
+        raw = torch._C._cuda_getCurrentRawStream(index)  # current_stream(index).cuda_stream, without the object
+    elif stream.device.index != index:
+        raise ValueError(f"a stream of {stream.device} for tensors on cuda:{index}")
+    else:
+        raw = stream.cuda_stream
+    if torch.cuda.current_device() == index:
+        rc = fn(*args, raw)
+    else:
+        with torch.cuda.device(index):
+            rc = fn(*args, raw)
+    _check(rc, where)
 
 
 def _scratch(nbytes: int, device, what: str):
@@ -532,6 +544,9 @@ class Sampling:
     top_k: object = None
     top_p: object = None
     min_p: object = None
+
+
+_NO_SAMPLING = Sampling()
 
 
 @dataclasses.dataclass
@@ -554,27 +569,26 @@ def sample(scores, rnd, out: SampleBuffers, params: Optional[Sampling] = None, s
     """One entry of every row of scores by temperature, top-k, top-p and min-p (hx_sample).  scores [rows, columns]:
     int32 (flow values), float32, float16 or bfloat16; rows may overlap or repeat (a stride of 0), entries of a row
     must be next to each other.  rnd: one 64-bit draw a row (int64 bit patterns)."""
-    torch = _torch()
-    types = {torch.int32: 0, torch.float32: 1, torch.float16: 2, torch.bfloat16: 3}
-    _need("scores", scores, tuple(types))
-    if scores.dim() != 2 or (scores.shape[1] > 1 and scores.stride(1) != 1):
-        raise ValueError("scores: two dimensions, the entries of a row next to each other")
-    R, dev = int(scores.shape[0]), scores.device
-    p = params if params is not None else Sampling()
-    _need("rnd", rnd, torch.int64, (R,), dev)
+    import torch
+    kind = {torch.int32: 0, torch.float32: 1, torch.float16: 2, torch.bfloat16: 3}.get(scores.dtype)
+    if kind is None or scores.dim() != 2 or (scores.shape[1] > 1 and scores.stride(1) != 1):
+        raise ValueError("scores: int32, float32, float16 or bfloat16 of two dimensions, the entries of a row next to "
+                         "each other")
+    R, N = scores.shape
+    gpu, row = _gpu_of("scores", scores), (R,)
+    p = params if params is not None else _NO_SAMPLING
+    _need("rnd", rnd, torch.int64, row, gpu)
+    _need("pick", out.pick, torch.int32, row, gpu)
+    _need("workspace", out.workspace, torch.uint8, out.workspace.shape, gpu)
     for name, t, dt in (("temperature", p.temperature, torch.float32), ("top_k", p.top_k, torch.int32),
                         ("top_p", p.top_p, torch.float32), ("min_p", p.min_p, torch.float32),
-                        ("pick", out.pick, torch.int32), ("logp", out.logp, torch.float32),
-                        ("kept", out.kept, torch.int32)):
+                        ("logp", out.logp, torch.float32), ("kept", out.kept, torch.int32)):
         if t is not None:
-            _need(name, t, dt, (R,), dev)
-    _need("workspace", out.workspace, torch.uint8, (out.workspace.numel(),), dev)
-    sc = hx_scores(R, int(scores.shape[1]), types[scores.dtype], int(scores.stride(0)), _ptr(scores))
+            _need(name, t, dt, row, gpu)
+    sc = hx_scores(R, N, kind, scores.stride(0), scores.data_ptr())
     sp = hx_sampling(_ptr(p.temperature), _ptr(p.top_k), _ptr(p.top_p), _ptr(p.min_p))
-    with torch.cuda.device(dev):
-        _check(lib().hx_sample(C.byref(sc), C.byref(sp), _ptr(rnd), _ptr(out.pick), _ptr(out.logp), _ptr(out.kept),
-                               _ptr(out.workspace), C.c_size_t(int(out.workspace.numel())), _own_stream(dev, stream)),
-               "hx_sample")
+    _launch(gpu, stream, "hx_sample", lib().hx_sample, C.byref(sc), C.byref(sp), rnd.data_ptr(), out.pick.data_ptr(),
+            _ptr(out.logp), _ptr(out.kept), out.workspace.data_ptr(), out.workspace.numel())
     return out
 
 
@@ -604,25 +618,25 @@ class RouteBuffers:
 def route_requests(net: FlowNetBuffers, kv_flow, rnd, out: RouteBuffers, cand: int = 0, stream=None) -> RouteBuffers:
     """A KV edge for every request, drawn in proportion to the flows of column cand (hx_route_requests).
     rnd: one 64-bit draw a request (int64 bit patterns)."""
-    torch = _torch()
+    import torch
     mp, md, mpd = net.dims
-    n, dev, N = int(rnd.shape[0]), rnd.device, int(net.n_p.shape[0])
-    _need("rnd", rnd, torch.int64, (n,))
-    _need("kv_flow", kv_flow, torch.int32, (mpd, N), dev)
-    for name, t, shape in (("n_p", net.n_p, (N,)), ("n_d", net.n_d, (N,)), ("prefill", out.prefill, (n,)),
-                           ("decode", out.decode, (n,)), ("p_order", out.p_order, (n,)),
-                           ("p_base", out.p_base, (mp + 1,)), ("d_order", out.d_order, (n,)),
-                           ("d_base", out.d_base, (md + 1,))):
+    n, N, gpu, i32 = rnd.numel(), net.n_p.numel(), _gpu_of("rnd", rnd), torch.int32
+    _need("rnd", rnd, torch.int64, (n,), gpu)
+    _need("kv_flow", kv_flow, i32, (mpd, N), gpu)
+    _need("n_p", net.n_p, i32, (N,), gpu)
+    _need("n_d", net.n_d, i32, (N,), gpu)
+    _need("prefill", out.prefill, i32, (n,), gpu)
+    _need("decode", out.decode, i32, (n,), gpu)
+    _need("workspace", out.workspace, torch.uint8, out.workspace.shape, gpu)
+    for name, t, m in (("p_order", out.p_order, n), ("p_base", out.p_base, mp + 1), ("d_order", out.d_order, n),
+                       ("d_base", out.d_base, md + 1)):
         if t is not None:
-            _need(name, t, torch.int32, shape, dev)
-    _need("workspace", out.workspace, torch.uint8, (out.workspace.numel(),), dev)
-    f = net.struct()
-    o = hx_routes(n, _ptr(out.prefill), _ptr(out.decode), _ptr(out.p_order), _ptr(out.p_base), _ptr(out.d_order),
-                  _ptr(out.d_base))
-    with torch.cuda.device(dev):
-        _check(lib().hx_route_requests(C.byref(f), C.c_int32(cand), _ptr(kv_flow), _ptr(rnd), C.byref(o),
-                                       _ptr(out.workspace), C.c_size_t(int(out.workspace.numel())),
-                                       _own_stream(dev, stream)), "hx_route_requests")
+            _need(name, t, i32, (m,), gpu)
+    f = hx_flownet(N, mp, md, mpd, net.n_p.data_ptr(), net.n_d.data_ptr())  # the call reads the counts alone
+    o = hx_routes(n, out.prefill.data_ptr(), out.decode.data_ptr(), _ptr(out.p_order), _ptr(out.p_base),
+                  _ptr(out.d_order), _ptr(out.d_base))
+    _launch(gpu, stream, "hx_route_requests", lib().hx_route_requests, C.byref(f), cand, kv_flow.data_ptr(),
+            rnd.data_ptr(), C.byref(o), out.workspace.data_ptr(), out.workspace.numel())
     return out
 
 
@@ -668,23 +682,27 @@ def kv_workspace(n_rows: int, n_replicas: int, device: str = "cuda"):
 
 
 def _kv_structs(pool: KvPool, rows: KvRows, workspace, free_out, held_out):
-    torch = _torch()
-    dev = rows.table.device
-    n, R = int(rows.replica.shape[0]), int(pool.free_count.shape[0])
+    import torch
+    table, i32 = rows.table, torch.int32
+    n, R, gpu = rows.replica.numel(), pool.free_count.numel(), _gpu_of("table", rows.table)
     free_out = pool.free_count if free_out is None else free_out
     held_out = rows.held if held_out is None else held_out
-    _need("table", rows.table, torch.int32)
-    if rows.table.dim() != 2 or rows.table.shape[0] != n or (rows.table.shape[1] > 1 and rows.table.stride(1) != 1):
-        raise ValueError("table: one row a request, the entries of a row next to each other")
-    width, stride = int(rows.table.shape[1]), int(rows.table.stride(0)) if n > 1 else int(rows.table.shape[1])
-    for name, t, shape in (("replica", rows.replica, (n,)), ("held", rows.held, (n,)), ("held_out", held_out, (n,)),
-                           ("base", pool.base, (R + 1,)), ("free_list", pool.free_list, (pool.free_list.numel(),)),
-                           ("free_count", pool.free_count, (R,)), ("free_out", free_out, (R,))):
-        _need(name, t, torch.int32, shape, dev)
-    _need("workspace", workspace, torch.uint8, (workspace.numel(),), dev)
-    return (hx_kv_pool(R, int(pool.block_size), _ptr(pool.base), _ptr(pool.free_list), _ptr(pool.free_count),
-                       _ptr(free_out)),
-            hx_kv_rows(n, width, stride, _ptr(rows.table), _ptr(rows.replica), _ptr(rows.held), _ptr(held_out)), dev, n)
+    if table.dtype is not i32 or table.dim() != 2 or table.shape[0] != n or (table.shape[1] > 1 and
+                                                                           table.stride(1) != 1):
+        raise ValueError("table: int32, one row a request, the entries of a row next to each other")
+    width = table.shape[1]
+    _need("replica", rows.replica, i32, (n,), gpu)
+    _need("held", rows.held, i32, (n,), gpu)
+    _need("held_out", held_out, i32, (n,), gpu)
+    _need("base", pool.base, i32, (R + 1,), gpu)
+    _need("free_list", pool.free_list, i32, (pool.free_list.numel(),), gpu)
+    _need("free_count", pool.free_count, i32, (R,), gpu)
+    _need("free_out", free_out, i32, (R,), gpu)
+    _need("workspace", workspace, torch.uint8, workspace.shape, gpu)
+    return (hx_kv_pool(R, pool.block_size, pool.base.data_ptr(), pool.free_list.data_ptr(), pool.free_count.data_ptr(),
+                       free_out.data_ptr()),
+            hx_kv_rows(n, width, table.stride(0) if n > 1 else width, table.data_ptr(), rows.replica.data_ptr(),
+                       rows.held.data_ptr(), held_out.data_ptr()), gpu, n)
 
 
 def kv_place(pool: KvPool, rows: KvRows, n_new, tok_base, slots, placed, workspace, free_out=None, held_out=None,
@@ -692,27 +710,24 @@ def kv_place(pool: KvPool, rows: KvRows, n_new, tok_base, slots, placed, workspa
     """Blocks and token slots for n_new (int32) more tokens of every row (hx_kv_place): tok_base int64 [rows + 1],
     slots int64, placed uint8 [rows].  The pool's free counts and the rows' lengths are updated in place unless
     free_out / held_out are given."""
-    torch = _torch()
-    p, r, dev, n = _kv_structs(pool, rows, workspace, free_out, held_out)
-    _need("n_new", n_new, torch.int32, (n,), dev)
-    _need("tok_base", tok_base, torch.int64, (n + 1,), dev)
-    _need("slots", slots, torch.int64, (slots.numel(),), dev)
-    _need("placed", placed, torch.uint8, (n,), dev)
-    with torch.cuda.device(dev):
-        _check(lib().hx_kv_place(C.byref(p), C.byref(r), _ptr(n_new), _ptr(tok_base), _ptr(slots),
-                                 C.c_int64(int(slots.numel())), _ptr(placed), _ptr(workspace),
-                                 C.c_size_t(int(workspace.numel())), _own_stream(dev, stream)), "hx_kv_place")
+    import torch
+    p, r, gpu, n = _kv_structs(pool, rows, workspace, free_out, held_out)
+    _need("n_new", n_new, torch.int32, (n,), gpu)
+    _need("tok_base", tok_base, torch.int64, (n + 1,), gpu)
+    _need("slots", slots, torch.int64, (slots.numel(),), gpu)
+    _need("placed", placed, torch.uint8, (n,), gpu)
+    _launch(gpu, stream, "hx_kv_place", lib().hx_kv_place, C.byref(p), C.byref(r), n_new.data_ptr(), tok_base.data_ptr(),
+            slots.data_ptr(), slots.numel(), placed.data_ptr(), workspace.data_ptr(), workspace.numel())
 
 
 def kv_release(pool: KvPool, rows: KvRows, done, workspace, free_out=None, held_out=None, stream=None) -> None:
     """The blocks of the rows with done (uint8) set back to their replicas (hx_kv_release); free counts and lengths as
     for kv_place."""
-    torch = _torch()
-    p, r, dev, n = _kv_structs(pool, rows, workspace, free_out, held_out)
-    _need("done", done, torch.uint8, (n,), dev)
-    with torch.cuda.device(dev):
-        _check(lib().hx_kv_release(C.byref(p), C.byref(r), _ptr(done), _ptr(workspace),
-                                   C.c_size_t(int(workspace.numel())), _own_stream(dev, stream)), "hx_kv_release")
+    import torch
+    p, r, gpu, n = _kv_structs(pool, rows, workspace, free_out, held_out)
+    _need("done", done, torch.uint8, (n,), gpu)
+    _launch(gpu, stream, "hx_kv_release", lib().hx_kv_release, C.byref(p), C.byref(r), done.data_ptr(),
+            workspace.data_ptr(), workspace.numel())
 
 
 @dataclasses.dataclass
