@@ -45,22 +45,23 @@ __device__ __forceinline__ void peer_sums(const Peers& p, uint32_t amount, u64* 
 
 struct KeySums {
     u64 wave[kWaves][kKeys];  // per-key totals of a wavefront's rows, then the sums before it
-    u64 run[kKeys];           // per-key totals of the tiles before
+    u64 run[kKeys];           // per-key totals of the rows before
 };
 
-// Sum of amount over the earlier rows with this lane's key, tiles before included; every lane of the
-// workgroup calls it.  The tile's totals are added to run.
-__device__ u64 key_prefix(KeySums& s, int key, bool has, uint32_t amount) {
-    const int tid = threadIdx.x, wave = tid >> 6;
-    for (int i = tid; i < kWaves * kKeys; i += kLanes) (&s.wave[0][0])[i] = 0;
-    __syncthreads();
+// Sum of amount over the earlier rows with this lane's key, the rows before (run) included; every lane of the
+// workgroup calls it, keys are below `keys`.  The 1,024 rows' totals are added to run.
+__device__ u64 key_prefix(KeySums& s, int keys, int key, bool has, uint32_t amount) {
+    const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
+    for (int k = lane; k < keys; k += 64) s.wave[wave][k] = 0;
     const Peers p(has ? key : 0, has);
     u64 below, all;
     peer_sums(p, has ? amount : 0u, &below, &all);
+    __builtin_amdgcn_wave_barrier();  // one wavefront's LDS accesses keep their order: the clearing is before this
     if (p.first()) s.wave[wave][key] = all;
     __syncthreads();
-    if (tid < kKeys) {
+    if (tid < keys) {
         u64 at = s.run[tid];
+#pragma unroll
         for (int w = 0; w < kWaves; ++w) {
             const u64 v = s.wave[w][tid];
             s.wave[w][tid] = at;
@@ -83,234 +84,567 @@ __device__ u64 block_scan(u64 v, u64* wave_sum) {
     }
     if (lane == 63) wave_sum[wave] = v;
     __syncthreads();
-    for (int w = 0; w < wave; ++w) v += wave_sum[w];
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w)
+        if (w < wave) v += wave_sum[w];
     __syncthreads();
     return v;
 }
 
+// Rows are worked on by chunks of whole 1,024s, a workgroup each, and at most kChunks of them, so that a chunk
+// can add up what the others counted by itself.
+constexpr int kChunks = 128;
+struct Chunks {
+    int32_t number, rows;
+    explicit Chunks(int32_t n) {
+        const int64_t tiles = ((int64_t)n + kLanes - 1) / kLanes;
+        const int64_t per = (tiles + kChunks - 1) / kChunks;
+        number = (int32_t)((tiles + per - 1) / per);
+        rows = (int32_t)(per * kLanes < n ? per * kLanes : n);
+    }
+};
+
 // ------------------------------------------------------------------ routes
 
+// Running sums of up to so many edges are kept in LDS, by every workgroup (in 32 of the 64 KB that a launch has
+// without asking for more); the networks of two sides of 64 nodes fit.
+constexpr int kEdgesLds = 4096;
+
 struct RouteArgs {
-    int32_t max_p, max_d, max_pd, nets, cand, n_req;
+    int32_t max_p, max_d, max_pd, nets, cand, n_req, chunk;
     const int32_t *n_p, *n_d, *kv_flow;
     const uint64_t* rnd;
     hx_routes o;
-    u64* ends;  // [max_pd] running sum of the flows
+    u64* ends;          // [max_pd] running sum of the flows, past kEdgesLds edges
+    uint32_t* counts;   // [2][chunks][kKeys] requests of each prefill and decode node, more chunks than one
 };
 
-__device__ void group(KeySums& s, u64* wave_sum, int nodes, int n_req, const int32_t* node, int32_t* order,
-                      int32_t* base) {
-    const int tid = threadIdx.x;
-    if (tid < kKeys) s.run[tid] = 0;
-    __syncthreads();
-    for (int i0 = 0; i0 < n_req; i0 += kLanes) {
-        const int v = i0 + tid < n_req ? node[i0 + tid] : -1;
-        key_prefix(s, v, v >= 0, 1u);
-    }
-    // where each node's run starts; requests without a route follow the last
-    const u64 mine = tid < nodes ? s.run[tid] : 0;
-    const u64 end = block_scan(mine, wave_sum);
-    if (tid < nodes) base[tid] = (int32_t)(end - mine);
-    if (tid == nodes) base[nodes] = (int32_t)end;
-    __syncthreads();
-    if (tid < kKeys) s.run[tid] = tid <= nodes ? end - mine : 0;
-    __syncthreads();
-    for (int i0 = 0; i0 < n_req; i0 += kLanes) {
-        const bool in = i0 + tid < n_req;
-        const int v = in ? node[i0 + tid] : 0;
-        const u64 at = key_prefix(s, v < 0 ? nodes : v, in, 1u);
-        if (in) order[at] = i0 + tid;
-    }
-}
-
-__global__ void __launch_bounds__(kLanes) route_kernel(RouteArgs a) {
-    __shared__ KeySums s;
-    __shared__ u64 wave_sum[kWaves];
-    __shared__ u64 carry;
+// Running sums of the flows, each lane summing edges next to each other.  Returns their total; D: decode nodes.
+__device__ u64 flow_ends(const RouteArgs& a, u64* ends, u64* wave_sum, int* edges_out, int* d_out) {
     const int tid = threadIdx.x;
     const int P = a.n_p[a.cand], D = a.n_d[a.cand];
     const bool ok = P >= 0 && D >= 0 && P <= a.max_p && D <= a.max_d && (int64_t)P * D <= a.max_pd;
     const int edges = ok ? P * D : 0;
-    if (tid == 0) carry = 0;
-    __syncthreads();
-    for (int e0 = 0; e0 < edges; e0 += kLanes) {
-        const int e = e0 + tid;
-        const int32_t f = e < edges ? a.kv_flow[(int64_t)e * a.nets + a.cand] : 0;
-        const u64 v = block_scan(f > 0 ? (u64)f : 0, wave_sum) + carry;
-        if (e < edges) a.ends[e] = v;
-        __syncthreads();
-        if (tid == kLanes - 1) carry = v;
-        __syncthreads();
+    const int per = (edges + kLanes - 1) / kLanes;
+    const int lo = tid * per < edges ? tid * per : edges, hi = lo + per < edges ? lo + per : edges;
+    u64 mine = 0;
+    for (int e = lo; e < hi; ++e) {
+        const int32_t f = a.kv_flow[(int64_t)e * a.nets + a.cand];
+        mine += f > 0 ? (u64)f : 0;
+        ends[e] = mine;
     }
-    const u64 total = carry;
-    for (int i = tid; i < a.n_req; i += kLanes) {
-        int p = -1, d = -1;
-        if (total > 0) {
-            const u64 t = __umul64hi((u64)a.rnd[i], total);
-            int lo = 0, hi = edges - 1;  // the first edge whose end is past t
-            while (lo < hi) {
-                const int mid = (lo + hi) / 2;
-                if (a.ends[mid] > t) hi = mid;
-                else lo = mid + 1;
-            }
-            p = lo / D;
-            d = lo - p * D;
+    const u64 scan = block_scan(mine, wave_sum);
+    for (int e = lo; e < hi; ++e) ends[e] += scan - mine;
+    __shared__ u64 total;
+    if (tid == kLanes - 1) total = scan;
+    __syncthreads();
+    *edges_out = edges;
+    *d_out = D;
+    return total;
+}
+
+// Request i's edge: the first one whose running sum is past floor(rnd F / 2^64).
+__device__ __forceinline__ void route_one(const RouteArgs& a, int i, const u64* ends, int edges, int D, u64 total,
+                                          int* p, int* d) {
+    *p = *d = -1;
+    if (total > 0) {
+        const u64 t = __umul64hi((u64)a.rnd[i], total);
+        int lo = 0, hi = edges - 1;
+        while (lo < hi) {
+            const int mid = (lo + hi) / 2;
+            if (ends[mid] > t) hi = mid;
+            else lo = mid + 1;
         }
-        a.o.prefill[i] = p;
-        a.o.decode[i] = d;
+        *p = lo / D;
+        *d = lo - *p * D;
+    }
+    a.o.prefill[i] = *p;
+    a.o.decode[i] = *d;
+}
+
+// Where each node's run starts, from the nodes' totals (run): base, and the starts in run; requests without a
+// route (key `nodes`) follow the last.
+__device__ void run_starts(KeySums& s, u64* wave_sum, int nodes, int32_t* base) {
+    const int tid = threadIdx.x;
+    const u64 mine = tid < nodes ? s.run[tid] : 0;
+    const u64 end = block_scan(mine, wave_sum);
+    if (base && tid <= nodes) base[tid] = (int32_t)(end - mine);
+    __syncthreads();
+    if (tid <= nodes) s.run[tid] = end - mine;
+    __syncthreads();
+}
+
+// All of it by one workgroup, up to 1,024 requests.
+template <bool kLds>
+__global__ void __launch_bounds__(kLanes) route_kernel(RouteArgs a) {
+    __shared__ u64 wave_sum[kWaves];
+    extern __shared__ u64 lds[];  // the running sums, and after them the lists' KeySums
+    u64* ends = kLds ? lds : a.ends;
+    KeySums& s = *reinterpret_cast<KeySums*>(lds);
+    const int tid = threadIdx.x;
+    int edges, D, p = -1, d = -1;
+    const u64 total = flow_ends(a, ends, wave_sum, &edges, &D);
+    const bool in = tid < a.n_req;
+    if (in) route_one(a, tid, ends, edges, D, total, &p, &d);
+    __syncthreads();
+#pragma unroll
+    for (int side = 0; side < 2; ++side) {
+        const int nodes = side ? a.max_d : a.max_p, node = side ? d : p;
+        int32_t* order = side ? a.o.d_order : a.o.p_order;
+        if (!order) continue;
+        if (tid <= nodes) s.run[tid] = 0;
+        __syncthreads();
+        // a first count gives the starts, after which a lane's place is its start and its rank
+        const u64 rank = key_prefix(s, nodes + 1, node < 0 ? nodes : node, in, 1u);
+        run_starts(s, wave_sum, nodes, side ? a.o.d_base : a.o.p_base);
+        if (in) order[s.run[node < 0 ? nodes : node] + rank] = tid;
+        __syncthreads();
+    }
+}
+
+// More requests: a chunk's edges and its counts of every node,
+template <bool kLds>
+__global__ void __launch_bounds__(kLanes) route_edges_kernel(RouteArgs a) {
+    __shared__ uint32_t count[2][kKeys];
+    __shared__ u64 wave_sum[kWaves];
+    extern __shared__ u64 lds_ends[];
+    const int tid = threadIdx.x;
+    int edges, D;
+    u64 total;
+    if (kLds) {
+        total = flow_ends(a, lds_ends, wave_sum, &edges, &D);
+    } else {
+        // written by the launch before; counts outside the arrays have no edges there either
+        const int P = a.n_p[a.cand];
+        D = a.n_d[a.cand];
+        edges = P >= 0 && D >= 0 && P <= a.max_p && D <= a.max_d && (int64_t)P * D <= a.max_pd ? P * D : 0;
+        total = edges ? a.ends[edges - 1] : 0;
+    }
+    if (tid < 2 * kKeys) (&count[0][0])[tid] = 0;
+    __syncthreads();
+    const int64_t i0 = (int64_t)blockIdx.x * a.chunk;
+    const int64_t i1 = i0 + a.chunk < a.n_req ? i0 + a.chunk : a.n_req;
+    for (int64_t i = i0 + tid; i < i1; i += kLanes) {
+        int p, d;
+        route_one(a, (int)i, kLds ? lds_ends : a.ends, edges, D, total, &p, &d);
+        if (p >= 0) {
+            atomicAdd(&count[0][p], 1u);
+            atomicAdd(&count[1][d], 1u);
+        }
     }
     __syncthreads();
-    if (a.o.p_order) group(s, wave_sum, a.max_p, a.n_req, a.o.prefill, a.o.p_order, a.o.p_base);
+    if (tid < 2 * kKeys) {
+        const int side = tid / kKeys, k = tid % kKeys;
+        a.counts[((int64_t)side * gridDim.x + blockIdx.x) * kKeys + k] = count[side][k];
+    }
+}
+
+__global__ void __launch_bounds__(kLanes) route_ends_kernel(RouteArgs a) {
+    __shared__ u64 wave_sum[kWaves];
+    int edges, D;
+    flow_ends(a, a.ends, wave_sum, &edges, &D);
+}
+
+// then its requests to their places: after all requests of earlier nodes, and the earlier chunks' of the same.
+__global__ void __launch_bounds__(kLanes) route_lists_kernel(RouteArgs a) {
+    __shared__ KeySums s;
+    __shared__ u64 wave_sum[kWaves];
+    const int tid = threadIdx.x, side = blockIdx.y;
+    const int nodes = side ? a.max_d : a.max_p;
+    const int32_t* node = side ? a.o.decode : a.o.prefill;
+    int32_t* order = side ? a.o.d_order : a.o.p_order;
+    if (!order) return;
+    u64 before = 0, all = 0;
+    if (tid < nodes) {
+        const uint32_t* c = a.counts + (int64_t)side * gridDim.x * kKeys + tid;
+        for (int t = 0; t < (int)gridDim.x; ++t) {
+            const uint32_t v = c[(int64_t)t * kKeys];
+            before += t < (int)blockIdx.x ? v : 0;
+            all += v;
+        }
+    }
+    if (tid <= nodes) s.run[tid] = all;
     __syncthreads();
-    if (a.o.d_order) group(s, wave_sum, a.max_d, a.n_req, a.o.decode, a.o.d_order, a.o.d_base);
+    run_starts(s, wave_sum, nodes, blockIdx.x == 0 ? (side ? a.o.d_base : a.o.p_base) : nullptr);
+    const int64_t i0 = (int64_t)blockIdx.x * a.chunk;
+    const int64_t i1 = i0 + a.chunk < a.n_req ? i0 + a.chunk : a.n_req;
+    // requests without a route: those of earlier chunks are what their nodes leave of i0
+    const u64 earlier = block_scan(before, wave_sum);
+    if (tid < nodes) s.run[tid] += before;
+    if (tid == kLanes - 1) s.run[nodes] += (u64)i0 - earlier;
+    __syncthreads();
+    for (int64_t i = i0; i < i1; i += kLanes) {
+        const bool in = i + tid < i1;
+        const int v = in ? node[i + tid] : 0;
+        const u64 at = key_prefix(s, nodes + 1, v < 0 ? nodes : v, in, 1u);
+        if (in) order[at] = (int32_t)(i + tid);
+    }
 }
 
 // ------------------------------------------------------------------ KV memory
 
-struct PlaceArgs {
+// A row of a call, as its tokens or blocks need it.
+struct KvRow {
+    int64_t top;   // place: free-list index of its first new block (the next ones below it); release: of its last
+    int32_t held;  // tokens before the call
+    int32_t number;  // place: 1 where served; release: blocks that go
+};
+
+struct KvArgs {
     hx_kv_pool p;
     hx_kv_rows r;
+    int32_t chunk, chunks;
     const int32_t* n_new;
     int64_t *tok_base, *slots;
     int64_t max_slots;
     uint8_t* placed;
+    const uint8_t* done;
+    KvRow* row;    // [n_rows]
+    u64* total;    // [chunks][kKeys] blocks of each replica's rows
+    u64* tokens;   // [chunks]
+    u64* moved;    // [kKeys] blocks taken or given
+    int64_t *free0, *room;  // [kKeys] entries free before, and left above them
 };
 
-// Entries of replica q's part of the free list, and how many of them are free.
-__device__ __forceinline__ int64_t room_of(const hx_kv_pool& p, int q) {
-    const int64_t c = (int64_t)p.base[q + 1] - p.base[q];
-    return c < 0 ? 0 : c;
-}
-__device__ __forceinline__ int64_t free_of(const hx_kv_pool& p, int q) {
-    const int64_t c = room_of(p, q), f = p.free_count[q];
-    return f < 0 ? 0 : f > c ? c : f;
+struct Replica {
+    int64_t free0, room;
+    __device__ __forceinline__ Replica(int64_t f, int64_t r) : free0(f), room(r) {}
+    __device__ __forceinline__ Replica(const hx_kv_pool& p, int q) {
+        const int64_t c = (int64_t)p.base[q + 1] - p.base[q], f = p.free_count[q];
+        const int64_t cap = c < 0 ? 0 : c;
+        free0 = f < 0 ? 0 : f > cap ? cap : f;
+        room = cap - free0;
+    }
+};
+
+// Row i's lengths and blocks.  place: need; release: the blocks that would go (rows count from the last).
+struct Demand {
+    int64_t held, add;
+    int q;
+    uint32_t blocks;
+    bool fits;
+    template <bool kPlace>
+    __device__ __forceinline__ void read(const KvArgs& a, int64_t i, bool in) {
+        const int64_t bs = a.p.block_size;
+        held = in ? a.r.held[i] : 0;
+        q = in ? a.r.replica[i] : -1;
+        fits = in && q >= 0 && q < a.p.n_replicas && held >= 0;
+        if (kPlace) {
+            const int64_t raw = in ? a.n_new[i] : 0;
+            add = raw < 0 ? 0 : raw;
+            fits = fits && raw >= 0 && held + add <= INT32_MAX;
+            // 32-bit divisions: held + add is below 2^31 wherever the quotient counts
+            const uint32_t b = (uint32_t)bs, b0 = ((uint32_t)held + b - 1) / b, b1 = ((uint32_t)(held + add) + b - 1) / b;
+            fits = fits && b1 <= (uint32_t)a.r.max_blocks;
+            blocks = fits ? b1 - b0 : 0u;
+        } else {
+            add = 0;
+            const uint32_t nb = ((uint32_t)held + (uint32_t)bs - 1) / (uint32_t)bs;
+            fits = fits && a.done[i] && nb <= (uint32_t)a.r.max_blocks;
+            blocks = fits ? nb : 0u;
+        }
+    }
+};
+
+// Totals of every chunk: blocks by replica, and tokens.
+template <bool kPlace>
+__global__ void __launch_bounds__(kLanes) kv_totals_kernel(KvArgs a) {
+    __shared__ u64 sum[kKeys], wave_sum[kWaves];
+    const int tid = threadIdx.x;
+    if (tid < kKeys) {
+        sum[tid] = 0;
+        if (blockIdx.x == 0 && tid < a.p.n_replicas) {
+            const Replica q(a.p, tid);
+            a.moved[tid] = 0;
+            a.free0[tid] = q.free0;
+            a.room[tid] = q.room;
+        }
+    }
+    __syncthreads();
+    const int64_t i0 = (int64_t)blockIdx.x * a.chunk;
+    const int64_t i1 = i0 + a.chunk < a.r.n_rows ? i0 + a.chunk : a.r.n_rows;
+    u64 tokens = 0;
+    for (int64_t i = i0 + tid; i < i1; i += kLanes) {
+        Demand d;
+        d.read<kPlace>(a, kPlace ? i : a.r.n_rows - 1 - i, true);
+        tokens += (u64)d.add;
+        if (d.blocks) atomicAdd(&sum[d.q], (u64)d.blocks);
+    }
+    tokens = block_scan(tokens, wave_sum);
+    if (tid == kLanes - 1) a.tokens[blockIdx.x] = tokens;
+    __syncthreads();
+    if (tid < a.p.n_replicas) a.total[(int64_t)blockIdx.x * kKeys + tid] = sum[tid];
 }
 
-__global__ void __launch_bounds__(kLanes) place_kernel(PlaceArgs a) {
+// Slot of token t (counted over all rows) of row i, which starts at token first: its block is the table's, or new
+// and entered into it by its first token.
+__device__ __forceinline__ int64_t slot_of(const KvArgs& a, int64_t i, const KvRow& row, int64_t t, int64_t first) {
+    if (!row.number) return -1;
+    const uint32_t b = (uint32_t)a.p.block_size, pos = (uint32_t)(row.held + (int32_t)(t - first));
+    const uint32_t col = pos / b, off = pos - col * b, b0 = ((uint32_t)row.held + b - 1) / b;
+    int32_t* entry = a.r.block_table + i * a.r.table_stride + col;
+    int32_t block;
+    if (col < b0) {
+        block = *entry;
+    } else {
+        block = a.p.free_list[row.top - (int64_t)(col - b0)];
+        if (off == 0) *entry = block;
+    }
+    return (int64_t)block * b + off;
+}
+
+constexpr int kFillHere = 4096;  // tokens that place's one workgroup fills in itself
+
+// The rows of a chunk, with the sums of the chunks before (kOne: the only one).  Fills the slots too where fill.
+template <bool kPlace, bool kOne>
+__global__ void __launch_bounds__(kLanes) kv_rows_kernel(KvArgs a, int fill) {
     __shared__ KeySums s;
     __shared__ u64 wave_sum[kWaves], carry;
-    __shared__ int64_t free0[kKeys];
-    __shared__ u64 taken[kKeys];
+    __shared__ int64_t free0[kKeys], limit[kKeys];
+    __shared__ u64 moved[kKeys];
+    __shared__ int32_t start[kOne ? kLanes : 1];  // kOne: the rows' first tokens and data, for the fill
+    __shared__ KvRow own[kOne ? kLanes : 1];
     const int tid = threadIdx.x, R = a.p.n_replicas;
-    const int64_t bs = a.p.block_size;
-    if (tid < kKeys) {
-        s.run[tid] = 0;
-        taken[tid] = 0;
-        free0[tid] = tid < R ? free_of(a.p, tid) : 0;
+    if (tid < R) {
+        u64 before = 0;
+        if (!kOne)
+            for (int t = 0; t < (int)blockIdx.x; ++t) before += a.total[(int64_t)t * kKeys + tid];
+        const Replica q = kOne ? Replica(a.p, tid) : Replica(a.free0[tid], a.room[tid]);
+        s.run[tid] = before;
+        moved[tid] = 0;
+        free0[tid] = q.free0;
+        limit[tid] = kPlace ? q.free0 : q.room;
     }
     if (tid == 0) carry = 0;
+    if (!kOne && kPlace) {
+        const u64 before = block_scan(tid < (int)blockIdx.x ? a.tokens[tid] : 0, wave_sum);  // at most kChunks <= kLanes
+        if (tid == kLanes - 1) carry = before;
+    }
     __syncthreads();
-    for (int i0 = 0; i0 < a.r.n_rows; i0 += kLanes) {
-        const int i = i0 + tid;
-        const bool in = i < a.r.n_rows;
-        const int64_t held = in ? a.r.held[i] : 0, raw = in ? a.n_new[i] : 0;
-        const int q = in ? a.r.replica[i] : -1;
-        const int64_t add = raw < 0 ? 0 : raw;
-        const u64 end = block_scan((u64)add, wave_sum) + carry;
-        __syncthreads();
-        if (tid == kLanes - 1) carry = end;
-        const int64_t tok = (int64_t)(end - (u64)add);
-        if (in && i == 0) a.tok_base[0] = 0;
-        if (in) a.tok_base[i + 1] = (int64_t)end;
-        const int64_t b0 = (held + bs - 1) / bs, b1 = (held + add + bs - 1) / bs;
-        const bool fits = in && q >= 0 && q < R && held >= 0 && raw >= 0 && held + add <= INT32_MAX &&
-                          b1 <= a.r.max_blocks && (int64_t)end <= a.max_slots;
-        const uint32_t need = fits ? (uint32_t)(b1 - b0) : 0u;
-        const u64 at = key_prefix(s, q, fits, need);
-        const bool served = fits && (need == 0 || (int64_t)(at + need) <= free0[q]);
-        if (in) {
-            a.placed[i] = served;
-            a.r.held_out[i] = (int32_t)(served ? held + add : held);
+    const int64_t i0 = (int64_t)blockIdx.x * a.chunk;
+    const int64_t i1 = i0 + a.chunk < a.r.n_rows ? i0 + a.chunk : a.r.n_rows;
+    for (int64_t i = i0; i < i1; i += kLanes) {
+        const bool in = i + tid < i1;
+        const int64_t at_row = kPlace ? i + tid : a.r.n_rows - 1 - (i + tid);
+        Demand d;
+        d.read<kPlace>(a, at_row, in);
+        u64 end = 0;
+        if (kPlace) {
+            end = block_scan((u64)d.add, wave_sum) + carry;
+            __syncthreads();
+            if (tid == kLanes - 1) carry = end;
+            if (in) a.tok_base[at_row + 1] = (int64_t)end;
+            if (in && at_row == 0) a.tok_base[0] = 0;
+            // rows past the slots: the rows after them are too, so what those would count does not matter
+            d.fits = d.fits && (int64_t)end <= a.max_slots;
+            d.blocks = d.fits ? d.blocks : 0u;
         }
-        if (served && need > 0) atomicMax(&taken[q], at + need);
+        const u64 at = key_prefix(s, R, d.q, d.fits, d.blocks);
+        const bool served = d.fits && (d.blocks == 0 || (int64_t)(at + d.blocks) <= limit[d.q]);
+        if (served && d.blocks) atomicMax(&moved[d.q], at + d.blocks);
         if (in) {
-            int32_t* table = a.r.block_table + (int64_t)i * a.r.table_stride;
-            const int32_t* top = served && need > 0 ? a.p.free_list + a.p.base[q] + free0[q] - 1 - (int64_t)at : nullptr;
-            if (served)
-                for (uint32_t c = 0; c < need; ++c) table[b0 + c] = top[-(int64_t)c];
-            for (int64_t t = 0; t < add && tok + t < a.max_slots; ++t) {
-                const int64_t pos = held + t;
-                a.slots[tok + t] = served ? table[pos / bs] * bs + pos % bs : -1;
+            const int64_t first = d.fits ? a.p.base[d.q] + free0[d.q] : 0;
+            KvRow row;
+            row.held = (int32_t)d.held;
+            if (kPlace) {
+                row.top = first - 1 - (int64_t)at;
+                row.number = served;
+                a.placed[at_row] = served;
+                a.r.held_out[at_row] = (int32_t)(served ? d.held + d.add : d.held);
+            } else {
+                row.top = first + (int64_t)at + d.blocks - 1;
+                row.number = served ? (int32_t)d.blocks : 0;
+                a.r.held_out[at_row] = served ? 0 : (int32_t)d.held;
+            }
+            if (kOne && kPlace && fill) {
+                const int64_t tok = (int64_t)end - d.add;
+                start[tid] = (int32_t)(tok < kFillHere ? tok : kFillHere);
+                own[tid] = row;
+            } else {
+                a.row[at_row] = row;
             }
         }
-        __syncthreads();
-    }
-    if (tid < R) a.p.free_out[tid] = (int32_t)(free0[tid] - (int64_t)taken[tid]);
-}
-
-struct ReleaseArgs {
-    hx_kv_pool p;
-    hx_kv_rows r;
-    const uint8_t* done;
-};
-
-// Rows in descending order: the last row's last block lands lowest.
-__global__ void __launch_bounds__(kLanes) release_kernel(ReleaseArgs a) {
-    __shared__ KeySums s;
-    __shared__ int64_t free0[kKeys], room[kKeys];
-    __shared__ u64 given[kKeys];
-    const int tid = threadIdx.x, R = a.p.n_replicas;
-    const int64_t bs = a.p.block_size;
-    if (tid < kKeys) {
-        s.run[tid] = 0;
-        given[tid] = 0;
-        free0[tid] = tid < R ? free_of(a.p, tid) : 0;
-        room[tid] = tid < R ? room_of(a.p, tid) - free0[tid] : 0;
     }
     __syncthreads();
-    for (int i0 = 0; i0 < a.r.n_rows; i0 += kLanes) {
-        const int i = a.r.n_rows - 1 - (i0 + tid);
-        const bool in = i >= 0;
-        const int64_t held = in ? a.r.held[i] : 0;
-        const int q = in ? a.r.replica[i] : -1;
-        const int64_t nb = (held + bs - 1) / bs;
-        const bool fits = in && a.done[i] && q >= 0 && q < R && held >= 0 && nb <= a.r.max_blocks;
-        const uint32_t blocks = fits ? (uint32_t)nb : 0u;
-        const u64 at = key_prefix(s, q, fits, blocks);
-        const bool goes = fits && (blocks == 0 || (int64_t)(at + blocks) <= room[q]);
-        if (in) a.r.held_out[i] = goes ? 0 : (int32_t)held;
-        if (goes && blocks > 0) {
-            atomicMax(&given[q], at + blocks);
-            const int32_t* table = a.r.block_table + (int64_t)i * a.r.table_stride;
-            int32_t* to = a.p.free_list + a.p.base[q] + free0[q] + (int64_t)at;
-            for (uint32_t c = 0; c < blocks; ++c) to[c] = table[blocks - 1 - c];
-        }
-        __syncthreads();
+    if (tid < R) {
+        if (kOne) a.p.free_out[tid] = (int32_t)(kPlace ? free0[tid] - (int64_t)moved[tid] : free0[tid] + (int64_t)moved[tid]);
+        else if (moved[tid]) atomicMax(&a.moved[tid], moved[tid]);
     }
-    if (tid < R) a.p.free_out[tid] = (int32_t)(free0[tid] + (int64_t)given[tid]);
+    if (kPlace && kOne && fill) {
+        const int tokens = (int)((int64_t)carry < a.max_slots ? (int64_t)carry : a.max_slots);
+        for (int t = tid; t < tokens; t += kLanes) {
+            int lo = 0, hi = a.r.n_rows - 1;  // the last row that starts at or before t
+            while (lo < hi) {
+                const int mid = (lo + hi + 1) / 2;
+                if (start[mid] <= t) lo = mid;
+                else hi = mid - 1;
+            }
+            a.slots[t] = slot_of(a, lo, own[lo], t, start[lo]);
+        }
+    }
+}
+
+__device__ __forceinline__ void write_free(const KvArgs& a, bool place) {
+    if (a.chunks > 1 && blockIdx.x == 0 && blockIdx.y == 0)
+        for (int q = threadIdx.x; q < a.p.n_replicas; q += blockDim.x)
+            a.p.free_out[q] = (int32_t)(place ? a.free0[q] - (int64_t)a.moved[q] : a.free0[q] + (int64_t)a.moved[q]);
+}
+
+// Slots of kFillTokens tokens.
+constexpr int kFillLanes = 256, kFillTokens = 2048;
+__global__ void __launch_bounds__(kFillLanes) place_fill_kernel(KvArgs a) {
+    write_free(a, true);
+    const int64_t n = a.tok_base[a.r.n_rows] < a.max_slots ? a.tok_base[a.r.n_rows] : a.max_slots;
+    const int64_t t0 = (int64_t)blockIdx.x * kFillTokens;
+    if (t0 >= n) return;
+    const int64_t t1 = t0 + kFillTokens < n ? t0 + kFillTokens : n;
+    // the last rows that start at or before the first and the last token
+    int64_t ends[2];
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+        const int64_t t = k ? t1 - 1 : t0;
+        int64_t lo = 0, hi = a.r.n_rows - 1;
+        while (lo < hi) {
+            const int64_t mid = (lo + hi + 1) / 2;
+            if (a.tok_base[mid] <= t) lo = mid;
+            else hi = mid - 1;
+        }
+        ends[k] = lo;
+    }
+    for (int64_t t = t0 + threadIdx.x; t < t1; t += kFillLanes) {
+        int64_t lo = ends[0], hi = ends[1];
+        while (lo < hi) {
+            const int64_t mid = (lo + hi + 1) / 2;
+            if (a.tok_base[mid] <= t) lo = mid;
+            else hi = mid - 1;
+        }
+        a.slots[t] = slot_of(a, lo, a.row[lo], t, a.tok_base[lo]);
+    }
+}
+
+// A wavefront copies kCopyBlocks blocks of one row at a time, the row's last block lowest.
+constexpr int kCopyLanes = 256, kCopyBlocks = 1024;
+__global__ void __launch_bounds__(kCopyLanes) release_copy_kernel(KvArgs a) {
+    write_free(a, false);
+    for (int64_t i = (int64_t)blockIdx.x * (kCopyLanes / 64) + (threadIdx.x >> 6); i < a.r.n_rows;
+         i += (int64_t)gridDim.x * (kCopyLanes / 64)) {
+        const KvRow row = a.row[i];
+        const int32_t* table = a.r.block_table + i * a.r.table_stride;
+        for (int64_t c0 = (int64_t)blockIdx.y * kCopyBlocks; c0 < row.number; c0 += (int64_t)gridDim.y * kCopyBlocks) {
+            const int64_t c1 = c0 + kCopyBlocks < row.number ? c0 + kCopyBlocks : row.number;
+#pragma unroll 4
+            for (int64_t c = c0 + (threadIdx.x & 63); c < c1; c += 64) a.p.free_list[row.top - c] = table[c];
+        }
+    }
+}
+
+size_t align256(size_t b) { return (b + 255) & ~(size_t)255; }
+
+struct KvScratch {
+    size_t row, total, tokens, moved, free0, room, bytes;
+    explicit KvScratch(int32_t n_rows) {
+        row = 0;
+        total = align256((size_t)n_rows * sizeof(KvRow));
+        tokens = total + sizeof(u64) * kChunks * kKeys;
+        moved = tokens + align256(sizeof(u64) * kChunks);
+        free0 = moved + sizeof(u64) * kKeys;
+        room = free0 + sizeof(int64_t) * kKeys;
+        bytes = room + sizeof(int64_t) * kKeys;
+    }
+};
+
+KvArgs kv_args(const hx_kv_pool& p, const hx_kv_rows& r, void* workspace) {
+    const Chunks c(r.n_rows);
+    const KvScratch w(r.n_rows);
+    unsigned char* b = static_cast<unsigned char*>(workspace);
+    KvArgs a{};
+    a.p = p;
+    a.r = r;
+    a.chunk = c.rows;
+    a.chunks = c.number;
+    a.row = reinterpret_cast<KvRow*>(b + w.row);
+    a.total = reinterpret_cast<u64*>(b + w.total);
+    a.tokens = reinterpret_cast<u64*>(b + w.tokens);
+    a.moved = reinterpret_cast<u64*>(b + w.moved);
+    a.free0 = reinterpret_cast<int64_t*>(b + w.free0);
+    a.room = reinterpret_cast<int64_t*>(b + w.room);
+    return a;
 }
 
 }  // namespace
 
-size_t route_workspace_bytes(int32_t, int32_t, int32_t max_pd, int32_t) {
-    return ((size_t)max_pd * sizeof(u64) + 255) & ~(size_t)255;
+size_t route_workspace_bytes(int32_t, int32_t, int32_t max_pd, int32_t n_req) {
+    const size_t ends = max_pd > kEdgesLds ? align256((size_t)max_pd * sizeof(u64)) : 0;
+    const Chunks c(n_req);
+    return ends + (c.number > 1 ? sizeof(uint32_t) * 2 * c.number * kKeys : 0) + 256;
 }
 
 hipError_t launch_route(const FlowNet& f, int32_t cand, const int32_t* kv_flow, const uint64_t* rnd, const hx_routes& o,
                         void* workspace, hipStream_t s) {
-    const RouteArgs a{f.max_p, f.max_d, f.max_pd, f.N, cand, o.n_req, f.n_p, f.n_d, kv_flow, rnd, o,
-                      static_cast<u64*>(workspace)};
+    const Chunks c(o.n_req);
+    const bool lds = f.max_pd <= kEdgesLds;
+    const size_t ends = lds ? 0 : align256((size_t)f.max_pd * sizeof(u64));
+    const size_t dyn = lds ? (size_t)f.max_pd * sizeof(u64) : 0;
+    const size_t one = dyn > sizeof(KeySums) ? dyn : sizeof(KeySums);
+    unsigned char* b = static_cast<unsigned char*>(workspace);
+    const RouteArgs a{f.max_p, f.max_d, f.max_pd, f.N, cand, o.n_req, c.rows, f.n_p, f.n_d, kv_flow, rnd, o,
+                      reinterpret_cast<u64*>(b), reinterpret_cast<uint32_t*>(b + ends)};
     prof_mark(kKRoute, false, s);
-    hipLaunchKernelGGL(route_kernel, dim3(1), dim3(kLanes), 0, s, a);
+    if (c.number == 1) {
+        if (lds) hipLaunchKernelGGL(route_kernel<true>, dim3(1), dim3(kLanes), one, s, a);
+        else hipLaunchKernelGGL(route_kernel<false>, dim3(1), dim3(kLanes), one, s, a);
+    } else {
+        if (!lds) hipLaunchKernelGGL(route_ends_kernel, dim3(1), dim3(kLanes), 0, s, a);
+        if (lds) hipLaunchKernelGGL(route_edges_kernel<true>, dim3(c.number), dim3(kLanes), dyn, s, a);
+        else hipLaunchKernelGGL(route_edges_kernel<false>, dim3(c.number), dim3(kLanes), 0, s, a);
+        if (o.p_order || o.d_order) hipLaunchKernelGGL(route_lists_kernel, dim3(c.number, 2), dim3(kLanes), 0, s, a);
+    }
     prof_mark(kKRoute, true, s);
     return hipGetLastError();
 }
 
-size_t kv_workspace_bytes(int32_t, int32_t) { return 256; }
+size_t kv_workspace_bytes(int32_t n_rows, int32_t) { return KvScratch(n_rows).bytes; }
 
 hipError_t launch_place(const hx_kv_pool& p, const hx_kv_rows& r, const int32_t* n_new, int64_t* tok_base,
-                        int64_t* slots, int64_t max_slots, uint8_t* placed, void*, hipStream_t s) {
-    const PlaceArgs a{p, r, n_new, tok_base, slots, max_slots, placed};
+                        int64_t* slots, int64_t max_slots, uint8_t* placed, void* workspace, hipStream_t s) {
+    KvArgs a = kv_args(p, r, workspace);
+    a.n_new = n_new;
+    a.tok_base = tok_base;
+    a.slots = slots;
+    a.max_slots = max_slots;
+    a.placed = placed;
     prof_mark(kKPlace, false, s);
-    hipLaunchKernelGGL(place_kernel, dim3(1), dim3(kLanes), 0, s, a);
+    const bool fill = a.chunks == 1 && max_slots <= kFillHere;
+    if (a.chunks == 1) {
+        hipLaunchKernelGGL((kv_rows_kernel<true, true>), dim3(1), dim3(kLanes), 0, s, a, (int)fill);
+    } else {
+        hipLaunchKernelGGL(kv_totals_kernel<true>, dim3(a.chunks), dim3(kLanes), 0, s, a);
+        hipLaunchKernelGGL((kv_rows_kernel<true, false>), dim3(a.chunks), dim3(kLanes), 0, s, a, 0);
+    }
+    if (!fill) {
+        // a grid has fewer than 2^32 lanes: up to 2^35 slots, whose 256 GiB are most of the memory
+        const int64_t fills = (max_slots + kFillTokens - 1) / kFillTokens;
+        hipLaunchKernelGGL(place_fill_kernel, dim3((unsigned)(fills < 1 ? 1 : fills)), dim3(kFillLanes), 0, s, a);
+    }
     prof_mark(kKPlace, true, s);
     return hipGetLastError();
 }
 
-hipError_t launch_release(const hx_kv_pool& p, const hx_kv_rows& r, const uint8_t* done, void*, hipStream_t s) {
-    const ReleaseArgs a{p, r, done};
+hipError_t launch_release(const hx_kv_pool& p, const hx_kv_rows& r, const uint8_t* done, void* workspace,
+                          hipStream_t s) {
+    KvArgs a = kv_args(p, r, workspace);
+    a.done = done;
     prof_mark(kKRelease, false, s);
-    hipLaunchKernelGGL(release_kernel, dim3(1), dim3(kLanes), 0, s, a);
+    if (a.chunks == 1) {
+        hipLaunchKernelGGL((kv_rows_kernel<false, true>), dim3(1), dim3(kLanes), 0, s, a, 0);
+    } else {
+        hipLaunchKernelGGL(kv_totals_kernel<false>, dim3(a.chunks), dim3(kLanes), 0, s, a);
+        hipLaunchKernelGGL((kv_rows_kernel<false, false>), dim3(a.chunks), dim3(kLanes), 0, s, a, 0);
+    }
+    const int64_t per = kCopyLanes / 64, x = (r.n_rows + per - 1) / per;
+    const int64_t y = (r.max_blocks + (int64_t)kCopyBlocks - 1) / kCopyBlocks;
+    const dim3 grid((unsigned)(x < 65536 ? x : 65536), (unsigned)(y < 64 ? y : 64));
+    hipLaunchKernelGGL(release_copy_kernel, grid, dim3(kCopyLanes), 0, s, a);
     prof_mark(kKRelease, true, s);
     return hipGetLastError();
 }
