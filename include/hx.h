@@ -439,8 +439,9 @@ int hx_partition_candidates(const hx_cluster *cluster, hx_model model, hx_worklo
 #define HX_SCORE_F32 1
 #define HX_SCORE_F16 2
 #define HX_SCORE_BF16 3
+#define HX_MAX_COLS (1 << 30)
 typedef struct hx_scores {
-    int32_t n_rows, n_cols;     /* R >= 1, N >= 1 */
+    int32_t n_rows, n_cols;     /* R >= 1, N in [1, HX_MAX_COLS] */
     int32_t type;               /* HX_SCORE_* */
     int64_t row_stride;         /* elements from one row to the next, >= 0 (0: every row reads the same scores) */
     const void *data;           /* [R][row_stride], aligned to its element */
@@ -467,7 +468,7 @@ typedef struct hx_sampling {
  *   pick [R] the index drawn; logp [R] nullable: z_pick - log S; kept [R] nullable: min(K, P, Q).
  * T = 0 gives the argmax, logp 0, kept 1.  A row that masks everything, or whose T is negative or not
  * finite, or whose p or q is NaN, gets pick -1, logp -inf, kept 0.
- *   workspace: hx_sample_workspace_bytes(R, N) bytes (0 for sizes below 1), 256-byte aligned, contents
+ *   workspace: hx_sample_workspace_bytes(R, N) bytes (0 for sizes out of range), 256-byte aligned, contents
  *   ignored on entry; calls that share it must not overlap. */
 size_t hx_sample_workspace_bytes(int32_t n_rows, int32_t n_cols);
 int hx_sample(const hx_scores *scores, const hx_sampling *params, const uint64_t *rnd, int32_t *pick, float *logp,

@@ -528,13 +528,13 @@ int hx_gather_candidates(int32_t n_gpus, const hx_candidates* src, const int32_t
 // ------------------------------------------------------------------ draws and dispatch
 
 size_t hx_sample_workspace_bytes(int32_t n_rows, int32_t n_cols) {
-    return n_rows < 1 || n_cols < 1 ? 0 : hx::sample_workspace_bytes(n_rows, n_cols);
+    return n_rows < 1 || n_cols < 1 || n_cols > HX_MAX_COLS ? 0 : hx::sample_workspace_bytes(n_rows, n_cols);
 }
 
 int hx_sample(const hx_scores* scores, const hx_sampling* params, const uint64_t* rnd, int32_t* pick, float* logp,
               int32_t* kept, void* workspace, size_t workspace_bytes, hipStream_t stream) {
     if (!scores || !params || !rnd || !pick || !scores->data) return HX_EINVAL;
-    if (scores->n_rows < 1 || scores->n_cols < 1 || scores->row_stride < 0) return HX_EINVAL;
+    if (scores->n_rows < 1 || scores->n_cols < 1 || scores->n_cols > HX_MAX_COLS || scores->row_stride < 0) return HX_EINVAL;
     if (scores->type < HX_SCORE_I32 || scores->type > HX_SCORE_BF16) return HX_EINVAL;
     const uintptr_t elem = scores->type == HX_SCORE_I32 || scores->type == HX_SCORE_F32 ? 4 : 2;
     if ((uintptr_t)scores->data & (elem - 1)) return HX_EINVAL;

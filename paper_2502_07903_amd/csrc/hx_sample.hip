@@ -3,7 +3,7 @@
 // Weights are w = exp((x - m) / T) in binary64, m the row's largest score (Exponent).  A row is read in
 // groups of 16 bytes (Row); a region is a run of groups that one wavefront walks, 64 groups at a time, and
 // the regions of a row follow each other in index order.  A draw is then: the regions' weights, their sum S
-// in order, the first region at which they pass t = u S, and the first entry of that region (pick_in_region).
+// in order, the first region at which they pass t = u S, and the first entry of that region (Pick).
 //
 // Without filters (all_kernel) the row is read once: a wavefront keeps its own largest score so far, sums
 // weights relative to it, and scales the sums when it grows (the ratio of two maxima is an exponential of
@@ -11,13 +11,16 @@
 // second launch (finish_kernel) joins them.
 //
 // With filters (cut_kernel, a workgroup per row): all three keep a prefix of the order (descending score,
-// ascending index), so the kept set is everything up to one entry (Cut).  That entry is found by counting,
-// for top-k, and by adding whole-number weights, for top-p (64-bit sums: no order of addition changes
-// them), in 2,048 bins of the distance from m; the entries of the bin in which the cut falls, if at most
-// kList, are ranked against each other in LDS, and otherwise the bin is split again by the keys' bits.
-// min-p's bound is a search over the keys.
+// ascending index), so the kept set is everything up to one entry's place in it.  That entry is found by
+// counting, for top-k, and by adding whole-number weights, for top-p (64-bit sums: no order of addition
+// changes them), in 2,048 bins of the distance from m.  The entries of the bin in which the cut falls, if
+// at most kList, go to a list in LDS, which is split by the bits of their places until a wavefront can rank
+// the rest; a longer bin is split again by the keys' bits over the row.  min-p's bound is a search over the
+// keys.
 #include <float.h>
 #include <math.h>
+
+#include <type_traits>
 
 #include "hx_internal.h"
 
@@ -28,33 +31,39 @@ using u64 = unsigned long long;
 
 // ------------------------------------------------------------------ scores
 
-// A score's 32-bit key has the scores' order (0: below all); V: entries of 16 bytes.
+// A score's 32-bit key has the scores' order; V: entries of 16 bytes; X: a score in registers.
 template <int kType>
 struct Scores;
 template <>
 struct Scores<HX_SCORE_I32> {
     using T = int32_t;
-    using X = int32_t;  // a score in registers
+    using X = int32_t;
     static constexpr int V = 4;
-    static constexpr X kMasked = INT32_MIN;
+    static constexpr X kMasked = INT32_MIN, kLeast = INT32_MIN + 1;  // the lowest score that is none
+    static __device__ __forceinline__ X clean(X x) { return x; }
     static __device__ __forceinline__ X widen(T x) { return x; }
     static __device__ __forceinline__ void unpack(const uint4& q, X (&v)[V]) {
         v[0] = (int32_t)q.x, v[1] = (int32_t)q.y, v[2] = (int32_t)q.z, v[3] = (int32_t)q.w;
     }
+    static __device__ __forceinline__ X larger(X a, X b) { return a > b ? a : b; }
     static __device__ __forceinline__ uint32_t key(X x) { return (uint32_t)x ^ 0x80000000u; }
     static __device__ __forceinline__ X value(uint32_t k) { return (int32_t)(k ^ 0x80000000u); }
+    static __device__ __forceinline__ X value_up(uint32_t k) { return value(k); }
     static __device__ __forceinline__ float below(X m, X x) { return (float)((uint32_t)m - (uint32_t)x); }
 };
-// Floats: NaN is masked (-inf) as it is read; keys are sign and magnitude in two's-complement order, -0 as +0.
+// Floats: NaN is masked (clean makes it -inf; unpack leaves it); keys are sign and magnitude in two's-complement order, -0 as +0.
 struct FloatScores {
     using X = float;
-    static constexpr X kMasked = -INFINITY;
+    static constexpr X kMasked = -INFINITY, kLeast = -FLT_MAX;
     static __device__ __forceinline__ X clean(float x) { return x > -INFINITY ? x : -INFINITY; }
+    static __device__ __forceinline__ X larger(X a, X b) { return fmaxf(a, b); }
     static __device__ __forceinline__ uint32_t key(X x) {
         const uint32_t b = __float_as_uint(x + 0.0f);
-        return b & 0x80000000u ? ~b : b | 0x80000000u;
+        return b ^ ((uint32_t)((int32_t)b >> 31) | 0x80000000u);
     }
     static __device__ __forceinline__ X value(uint32_t k) { return __uint_as_float(k & 0x80000000u ? k ^ 0x80000000u : ~k); }
+    // The largest score whose key is at most k: the key of -0, which no score has, would compare equal to +0.
+    static __device__ __forceinline__ X value_up(uint32_t k) { return value(k == 0x7FFFFFFFu ? k - 1 : k); }
     static __device__ __forceinline__ float below(X m, X x) { return m - x; }
 };
 template <>
@@ -63,23 +72,24 @@ struct Scores<HX_SCORE_F32> : FloatScores {
     static constexpr int V = 4;
     static __device__ __forceinline__ X widen(T x) { return clean(x); }
     static __device__ __forceinline__ void unpack(const uint4& q, X (&v)[V]) {
-        v[0] = clean(__uint_as_float(q.x)), v[1] = clean(__uint_as_float(q.y));
-        v[2] = clean(__uint_as_float(q.z)), v[3] = clean(__uint_as_float(q.w));
+        v[0] = __uint_as_float(q.x), v[1] = __uint_as_float(q.y);
+        v[2] = __uint_as_float(q.z), v[3] = __uint_as_float(q.w);
     }
 };
 template <>
 struct Scores<HX_SCORE_F16> : FloatScores {
     using T = uint16_t;
     static constexpr int V = 8;
-    static __device__ __forceinline__ X widen(T x) {
+    static __device__ __forceinline__ X raw(T x) {
         _Float16 h;
         __builtin_memcpy(&h, &x, 2);
-        return clean((float)h);
+        return (float)h;
     }
+    static __device__ __forceinline__ X widen(T x) { return clean(raw(x)); }
     static __device__ __forceinline__ void unpack(const uint4& q, X (&v)[V]) {
         const uint32_t w[4] = {q.x, q.y, q.z, q.w};
 #pragma unroll
-        for (int i = 0; i < 4; ++i) v[2 * i] = widen((T)w[i]), v[2 * i + 1] = widen((T)(w[i] >> 16));
+        for (int i = 0; i < 4; ++i) v[2 * i] = raw((T)w[i]), v[2 * i + 1] = raw((T)(w[i] >> 16));
     }
 };
 template <>
@@ -91,83 +101,152 @@ struct Scores<HX_SCORE_BF16> : FloatScores {
         const uint32_t w[4] = {q.x, q.y, q.z, q.w};
 #pragma unroll
         for (int i = 0; i < 4; ++i)
-            v[2 * i] = clean(__uint_as_float(w[i] << 16)), v[2 * i + 1] = clean(__uint_as_float(w[i] & 0xffff0000u));
+            v[2 * i] = __uint_as_float(w[i] << 16), v[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
     }
 };
 
 // w = exp((x - m) / T) as 2^(d c), d = x - m, c = log2(e) / T: d c = n + f with n whole and |f| <= 1/2, and
 // 2^f = 1 + f q(f), q the interpolation of (2^f - 1) / f at the ten Chebyshev nodes of [-1/2, 1/2] (computed
-// in 80 digits; 2^f is off by 6e-16 at most).  Masked scores (-inf) get n = -2000 and weight 0.
+// in 80 digits; 2^f is off by 6e-16 at most).  Masked scores (-inf) end at d c = -2000, whose weight is 0.
+// n comes from adding 1.5 2^52, which leaves it in the sum's low bits.  18 binary64 operations; several scores
+// are worked on side by side, step by step, since one's steps depend on each other.
 struct Exponent {
-    double m, c;
-    bool infinite;  // m = +inf: entries equal to it have d = 0
+    double m, c, least;  // least: d where d c = -2000
+    double lead;         // q's first coefficient, kept in vector registers: an fma reads one scalar operand
+    int infinite;        // m = +inf: entries equal to it have d = 0
     template <class X>
     __device__ __forceinline__ void set(X top, double scale) {
         m = (double)top;
         c = scale;
-        infinite = m > DBL_MAX;
+        infinite = __builtin_amdgcn_readfirstlane(m > DBL_MAX);
         if (infinite) m = 0x1p200;  // every finite score is infinitely far below
+        least = -2000.0 / scale;
+        lead = 0x1.e5e9f548e5725p-28;
+        asm("" : "+v"(lead));
     }
-    static __device__ __forceinline__ double pow2(double y) {
-        y = fmax(y, -2000.0);
-        const double n = rint(y), f = y - n;
-        double q = 0x1.e5e9f548e5725p-28;
-        q = fma(q, f, 0x1.b6571de2f2351p-24);
-        q = fma(q, f, 0x1.62bfe46117445p-20);
-        q = fma(q, f, 0x1.ffcb76789860fp-17);
-        q = fma(q, f, 0x1.4309130378460p-13);
-        q = fma(q, f, 0x1.5d87fe908f88ap-10);
-        q = fma(q, f, 0x1.3b2ab6fba385fp-7);
-        q = fma(q, f, 0x1.c6b08d7044119p-5);
-        q = fma(q, f, 0x1.ebfbdff82c590p-3);
-        q = fma(q, f, 0x1.62e42fefa39f7p-1);
-        return ldexp(fma(q, f, 1.0), (int)n);
+    // kAbove: scores may be above m, to weights of infinity.
+    template <bool kAbove = false, int N, class X>
+    __device__ __forceinline__ void weights(const X (&x)[N], double (&w)[N]) const {
+        constexpr int M = N < 4 ? N : 4;  // side by side
+#pragma unroll
+        for (int b = 0; b < N; b += M) some_weights<kAbove, M>(x + b, w + b);
     }
-    __device__ __forceinline__ double weight(float x) const {
-        double d = (double)x - m;
-        if (infinite) d = fmin(d, 0.0);
-        return pow2(d * c);
+    template <bool kAbove, int M, class X>
+    __device__ __forceinline__ void some_weights(const X* x, double* w) const {
+        double d[M], t[M], q[M];
+#pragma unroll
+        for (int e = 0; e < M; ++e) d[e] = fmax((double)x[e] - m, least);
+        if (kAbove) {
+#pragma unroll
+            for (int e = 0; e < M; ++e) d[e] = fmin(d[e], -least);
+        }
+        if (__builtin_amdgcn_readfirstlane(infinite)) {  // the same in every lane: a branch, not a mask
+#pragma unroll
+            for (int e = 0; e < M; ++e) d[e] = fmin(d[e], 0.0);
+        }
+#pragma unroll
+        for (int e = 0; e < M; ++e) t[e] = fma(d[e], c, 0x1.8p52);
+#pragma unroll
+        for (int e = 0; e < M; ++e) d[e] = fma(d[e], c, -(t[e] - 0x1.8p52));
+        constexpr double k[9] = {0x1.b6571de2f2351p-24, 0x1.62bfe46117445p-20, 0x1.ffcb76789860fp-17,
+                                 0x1.4309130378460p-13, 0x1.5d87fe908f88ap-10, 0x1.3b2ab6fba385fp-7,
+                                 0x1.c6b08d7044119p-5,  0x1.ebfbdff82c590p-3,  0x1.62e42fefa39f7p-1};
+#pragma unroll
+        for (int e = 0; e < M; ++e) q[e] = lead;
+#pragma unroll
+        for (int i = 0; i < 9; ++i) {
+#pragma unroll
+            for (int e = 0; e < M; ++e) q[e] = fma(q[e], d[e], k[i]);
+        }
+#pragma unroll
+        for (int e = 0; e < M; ++e) {
+            w[e] = ldexp(fma(q[e], d[e], 1.0), (int)(uint32_t)__double_as_longlong(t[e]));
+            if (std::is_same<X, int32_t>::value) w[e] = x[e] == (X)INT32_MIN ? 0.0 : w[e];
+        }
     }
-    __device__ __forceinline__ double weight(int32_t x) const {
-        const double w = pow2(((double)x - m) * c);
-        return x == INT32_MIN ? 0.0 : w;
+    template <class X>
+    __device__ __forceinline__ double weight(X x) const {
+        const X one[1] = {x};
+        double w[1];
+        weights(one, w);
+        return w[0];
     }
 };
 
 // ------------------------------------------------------------------ a row
 
+__device__ __forceinline__ int wave_index() { return __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)); }
+
+__device__ const uint4 kNoEntries = {};
+// Said to be global memory: a load that could be of LDS waits for both kinds.
+typedef uint32_t Words __attribute__((ext_vector_type(4)));
+using Group = const __attribute__((address_space(1))) Words;
+
 template <class S>
 struct Row {
     static constexpr int V = S::V;
+    using X = typename S::X;
     const typename S::T* x;
-    int n, lead;     // entries; those of the first 16 bytes that precede the row
-    int64_t groups;  // of 16 aligned bytes
+    int n, lead;  // entries; those of the first 16 bytes that precede the row
+    int groups;   // of 16 aligned bytes (n is at most 2^30: indices of groups and entries fit 32 bits)
+    int whole_lo, whole_hi;  // groups [whole_lo, whole_hi] lie within the row
+    Group* from;             // group 0; kNoEntries for a row without a whole group
     __device__ __forceinline__ Row(const SampleArgs& a, int64_t r) {
         x = static_cast<const typename S::T*>(a.data) + r * a.stride;
         n = a.N;
         lead = (int)(((uintptr_t)x & 15) / sizeof(typename S::T));
-        groups = ((int64_t)n + lead + V - 1) / V;
+        groups = (n + lead + V - 1) / V;
+        whole_lo = lead > 0 ? 1 : 0;
+        whole_hi = (n + lead) / V - 1;
+        from = (Group*)((uintptr_t)x & ~(uintptr_t)15);
+        if (whole_hi < whole_lo) from = (Group*)(uintptr_t)&kNoEntries;
     }
-    __device__ __forceinline__ int64_t first(int64_t g) const { return g * V - lead; }  // index of its first entry
-    // Entries of group g; those outside the row are masked, and not read.
-    __device__ __forceinline__ void load(int64_t g, typename S::X (&v)[V]) const {
-        const int64_t i = first(g);
-        if (i >= 0 && i + V <= n) {
-            S::unpack(*reinterpret_cast<const uint4*>(x + i), v);
-        } else {
+    __device__ __forceinline__ int first(int g) const { return g * V - lead; }  // index of its first entry
+    // The 16 bytes of group g, or of the whole group nearest to it: a load that no branch surrounds, so that it can be
+    // in flight while the group before it is worked on.
+    __device__ __forceinline__ uint4 fetch(int g) const {
+        const int w = g > whole_hi ? whole_hi : g;
+        const auto q = from[whole_hi < whole_lo ? 0 : w < whole_lo ? whole_lo : w];
+        return uint4{q.x, q.y, q.z, q.w};
+    }
+    // Entries of group g, fetched as q, of a region that ends at hi; those outside the row and the region are masked,
+    // and not read.
+    template <bool kClean = true>
+    __device__ __forceinline__ void entries(int g, int hi, const uint4& q, X (&v)[V]) const {
+        S::unpack(q, v);
+        if (kClean) {
 #pragma unroll
-            for (int e = 0; e < V; ++e) v[e] = i + e >= 0 && i + e < n ? S::widen(x[i + e]) : S::kMasked;
+            for (int e = 0; e < V; ++e) v[e] = S::clean(v[e]);
+        }
+        if (g >= hi || g < whole_lo || g > whole_hi) {
+            const int i = first(g);
+#pragma unroll
+            for (int e = 0; e < V; ++e) v[e] = g < hi && i + e >= 0 && i + e < n ? S::widen(x[i + e]) : S::kMasked;
+        }
+    }
+    // body(entries, index of the first) for a wavefront's groups [lo, hi), 64 at a time and all lanes together (masked
+    // entries where a lane has no group), the next 64 groups being fetched meanwhile.  Without kClean, NaN stays.
+    template <bool kClean = true, class B>
+    __device__ __forceinline__ void walk(int lo, int hi, B body) const {
+        const int lane = threadIdx.x & 63;
+        uint4 next = fetch(lo + lane);
+        for (int g = lo + lane; g - lane < hi; g += 64) {
+            const uint4 q = next;
+            next = fetch(g + 64);
+            X v[V];
+            entries<kClean>(g, hi, q, v);
+            body(v, first(g));
         }
     }
 };
 
 // Groups [lo, hi) of region k of a row's `regions`: whole wavefronts' worth, in index order.
 struct Region {
-    int64_t lo, hi;
-    __device__ __forceinline__ Region(int64_t groups, int regions, int k) {
-        const int64_t per = (groups + (int64_t)regions * 64 - 1) / ((int64_t)regions * 64) * 64;
-        lo = per * k < groups ? per * k : groups;
-        hi = lo + per < groups ? lo + per : groups;
+    int lo, hi;
+    __device__ __forceinline__ Region(int groups, int regions, int k) {
+        const int per = (groups + regions * 64 - 1) / (regions * 64) * 64;
+        lo = k < (groups + per - 1) / per ? per * k : groups;
+        hi = groups - lo > per ? lo + per : groups;
     }
 };
 
@@ -191,14 +270,10 @@ __device__ __forceinline__ void write_nothing(const SampleArgs& a, int64_t r) {
     if (a.kept) a.kept[r] = 0;
 }
 
-// ------------------------------------------------------------------ wavefront and workgroup sums
+// ------------------------------------------------------------------ wavefront sums
 
 __device__ __forceinline__ double wave_sum(double v) {
     for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o, 64);
-    return v;
-}
-__device__ __forceinline__ uint32_t wave_sum(uint32_t v) {
-    for (int o = 32; o > 0; o >>= 1) v += (uint32_t)__shfl_xor((int)v, o, 64);
     return v;
 }
 template <class X>
@@ -220,11 +295,23 @@ __device__ __forceinline__ A wave_scan(A v) {  // inclusive
 
 // ------------------------------------------------------------------ the draw
 
-// What a region adds: its largest score's key, the weight relative to that score (to the row's in
-// cut_kernel), and the number of entries.
+// What a region adds: the weight of its entries, relative to the score of `key`, and their number.
 struct Part {
     double weight;
     uint32_t key, count;
+};
+
+// The end of a row's draw: the entry found, the kept entries' weight and number.
+struct Draw {
+    const SampleArgs& a;
+    int64_t r;
+    double m, T, sum;
+    u64 kept;
+    __device__ __forceinline__ void write(int index, double v) const {
+        a.pick[r] = index;
+        if (a.kept) a.kept[r] = (int32_t)kept;
+        if (a.logp) a.logp[r] = T == 0.0 ? 0.0f : (float)((v == m ? 0.0 : (v - m) / T) - log(sum));
+    }
 };
 
 template <int kLanes>
@@ -233,42 +320,40 @@ struct PickShared {
     int found[kLanes / 64], last[kLanes / 64];
 };
 
-// The first kept entry of groups [lo, hi) up to which the weights sum to more than t, or the last one with
-// weight (which rounding can leave as the only choice).  weight(v, index): 0 for entries that are not kept.
-// Every lane of the workgroup calls it, and gets the answer.
+// The first entry of groups [lo, hi) up to which the weights sum to more than t, or the last one with weight
+// (which rounding can leave as the only choice), to the row's outputs.  weights(entries, index of the first, w): 0 for
+// entries that are not kept.  Every lane of the workgroup calls it; some entry has weight.
 template <int kLanes, class S, class W>
-__device__ int64_t pick_in_region(const Row<S>& row, const Region& g, double t, W weight, PickShared<kLanes>& sh) {
-    const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
+__device__ void pick_in_region(const Row<S>& row, const Region& g, double t, const Draw& draw, W weights,
+                               PickShared<kLanes>& sh) {
+    constexpr int kWaves = kLanes / 64;
+    const int wave = wave_index(), lane = threadIdx.x & 63;
     double run = 0.0;
-    int64_t last = -1;
-    for (int64_t g0 = g.lo; g0 < g.hi; g0 += kLanes) {
+    int last = -1;
+    for (int g0 = g.lo; g0 < g.hi; g0 += kLanes) {
+        const int at = g0 + (int)threadIdx.x;
         typename S::X v[S::V];
         double w[S::V], mine = 0.0;
-        const int64_t at = row.first(g0 + tid);
         int own = -1;
-        if (g0 + tid < g.hi) {
-            row.load(g0 + tid, v);
+        row.entries(at, g.hi, row.fetch(at), v);
+        weights(v, row.first(at), w);
 #pragma unroll
-            for (int e = 0; e < S::V; ++e) {
-                w[e] = weight(v[e], at + e);
-                mine += w[e];
-                if (w[e] > 0.0) own = e;
-            }
+        for (int e = 0; e < S::V; ++e) {
+            mine += w[e];
+            if (w[e] > 0.0) own = e;
         }
         const double scan = wave_scan(mine);
-        if (lane == 63) sh.wave[wave] = scan;
         const u64 has = __ballot(own >= 0);
         const int top = has ? 63 - __clzll(has) : 0;
         const int top_e = __shfl(own, top, 64);
-        if (lane == 0) sh.last[wave] = has ? (wave * 64 + top) * S::V + top_e : -1;
+        if (lane == 63) {
+            sh.wave[wave] = scan;
+            sh.last[wave] = has ? row.first(g0 + wave * 64 + top) + top_e : -1;
+        }
         __syncthreads();
-        double before = run;
-        for (int k = 0; k < wave; ++k) before += sh.wave[k];
-        double total = run;
-        for (int k = 0; k < kLanes / 64; ++k) total += sh.wave[k];
-        // an entry is past t when the sum up to it is; the first lane that holds one
+        for (int k = 0; k < wave; ++k) run += sh.wave[k];
+        double sum = run + (scan - mine);
         int e_found = -1;
-        double sum = before + (scan - mine);
         if (own >= 0) {
 #pragma unroll
             for (int e = 0; e < S::V; ++e) {
@@ -276,98 +361,140 @@ __device__ int64_t pick_in_region(const Row<S>& row, const Region& g, double t, 
                 if (e_found < 0 && w[e] > 0.0 && sum > t) e_found = e;
             }
         }
+        for (int k = wave; k < kWaves; ++k) run += sh.wave[k];
         const u64 past = __ballot(e_found >= 0);
-        const int first = past ? __ffsll(past) - 1 : 0;
-        const int first_e = __shfl(e_found, first, 64);
-        if (lane == 0) sh.found[wave] = past ? (wave * 64 + first) * S::V + first_e : -1;
+        const int first = past ? __ffsll(past) - 1 : 64;
+        if (lane == 0) sh.found[wave] = first;
         __syncthreads();
-        const int64_t base = row.first(g0);
-        int64_t found = -1;
-        for (int k = kLanes / 64 - 1; k >= 0; --k) {
-            if (sh.found[k] >= 0) found = base + sh.found[k];
+        int hit = kWaves;
+        for (int k = kWaves - 1; k >= 0; --k) {
+            if (sh.found[k] < 64) hit = k;
         }
-        for (int k = 0; k < kLanes / 64; ++k)
-            if (sh.last[k] >= 0) last = base + sh.last[k];
+        for (int k = 0; k < kWaves; ++k)
+            if (sh.last[k] >= 0) last = sh.last[k];
+        if (hit < kWaves) {
+            if (wave == hit && lane == first) {
+                double value = 0.0;
+#pragma unroll
+                for (int e = 0; e < S::V; ++e)
+                    if (e == e_found) value = (double)v[e];
+                draw.write(row.first(at) + e_found, value);
+            }
+            return;
+        }
         __syncthreads();
-        if (found >= 0) return found;
-        run = total;
     }
-    return last;
+    if (threadIdx.x == 0) draw.write(last, (double)S::widen(row.x[last]));
 }
 
 // ------------------------------------------------------------------ no filters
 
 constexpr int kAllLanes = 256, kAllWaves = kAllLanes / 64;
+// Regions of a wavefront where the workgroup has the whole row, since the draw reads one of them again; a short row's
+// is small as it is.
+constexpr int kAllRegions = 8, kShortRow = 8192;
 constexpr int kFinishLanes = 256;
 
-// Sum of a wavefront's groups [lo, hi) relative to the largest of them, in one pass.
+// The largest of the lanes' entries.
 template <class S>
-__device__ Part sum_region(const Row<S>& row, const Region& g, double scale) {
-    const int lane = threadIdx.x & 63;
-    typename S::X top = S::kMasked;
-    Exponent ex;
-    ex.set(top, scale);
-    double sum = 0.0;
-    uint32_t count = 0;
-    for (int64_t g0 = g.lo; g0 < g.hi; g0 += 64) {
-        typename S::X v[S::V];
-        if (g0 + lane < g.hi) {
-            row.load(g0 + lane, v);
-        } else {
+__device__ __forceinline__ typename S::X wave_most(const typename S::X (&v)[S::V]) {
+    typename S::X most = S::kMasked;
 #pragma unroll
-            for (int e = 0; e < S::V; ++e) v[e] = S::kMasked;
-        }
-        typename S::X most = v[0];
-#pragma unroll
-        for (int e = 1; e < S::V; ++e) most = v[e] > most ? v[e] : most;
-        if (__any(most > top)) {
-            const typename S::X grown = wave_max(most);
-            ex.set(grown, scale);
-            if (top != S::kMasked) sum *= ex.weight(top);
-            top = grown;
-        }
-#pragma unroll
-        for (int e = 0; e < S::V; ++e) {
-            sum += ex.weight(v[e]);
-            count += v[e] != S::kMasked;
-        }
-    }
-    return Part{wave_sum(sum), S::key(top), wave_sum(count)};
+    for (int e = 0; e < S::V; ++e) most = S::larger(most, v[e]);
+    return wave_max(most);
 }
 
-// The row's draw from its regions' parts, in parts[0 .. regions).  parts' weights are scaled to the row's
-// largest score by the lanes, in place in scaled[].
+// Weights of a wavefront's regions k0 .. k0 + n - 1 in one pass, to parts: relative to one of its own scores (Part's
+// key), the largest of the first 64 groups that hold any, and a larger one from where the weights pass 2^500.
+template <class S>
+__device__ void sum_regions(const Row<S>& row, int regions, int k0, int n, const Parameters& par, Part* parts) {
+    using X = typename S::X;
+    const Region first(row.groups, regions, k0), last(row.groups, regions, k0 + n - 1);
+    const int per = first.hi - first.lo, lane = threadIdx.x & 63;
+    const bool greedy = par.T == 0.0f;
+    const double scale = greedy ? 1.0 : par.scale();
+    X ref = S::kMasked;
+    Exponent ex;
+    ex.set(ref, scale);
+    double sum = 0.0;
+    uint32_t count = 0;  // of the wavefront
+    int k = 0, end = first.hi, g0 = first.lo;
+    const auto close = [&] {  // region k is done
+        if (greedy) ref = wave_max(ref);
+        const double total = greedy ? 1.0 : wave_sum(sum);
+        if (lane == 0) parts[k] = Part{total, S::key(ref), count};
+        if (greedy) ref = S::kMasked;
+        sum = 0.0;
+        count = 0;
+        ++k;
+        end += per;
+    };
+    row.template walk<false>(first.lo, last.hi, [&](const X (&v)[S::V], int) {
+        if (g0 >= end) close();
+        g0 += 64;
+#pragma unroll
+        for (int e = 0; e < S::V; ++e) count += __popcll(__ballot(v[e] >= S::kLeast));  // false for NaN
+        if (greedy) {
+#pragma unroll
+            for (int e = 0; e < S::V; ++e) ref = v[e] > ref ? v[e] : ref;
+            return;
+        }
+        if (ref == S::kMasked) {
+            ref = wave_most<S>(v);
+            if (ref == S::kMasked) return;
+            ex.set(ref, scale);
+        }
+        double w[S::V], here = 0.0;
+        ex.template weights<true>(v, w);
+#pragma unroll
+        for (int e = 0; e < S::V; ++e) here += w[e];
+        if (__any(!(here < 0x1p500))) {
+            // the earlier regions' parts keep their own score
+            const X old = ref;
+            ref = wave_most<S>(v);
+            ex.set(ref, scale);
+            sum *= ex.weight(old);
+            ex.weights(v, w);
+            here = 0.0;
+#pragma unroll
+            for (int e = 0; e < S::V; ++e) here += w[e];
+        }
+        sum += here;
+    });
+    while (k < n) close();
+}
+
+// The row's draw from its regions' parts; scaled: room for their weights relative to the row's largest score.
 template <int kLanes, class S>
 __device__ void finish_row(const SampleArgs& a, int64_t r, const Row<S>& row, const Parameters& par, const Part* parts,
                            int regions, double* scaled, PickShared<kLanes>& sh) {
-    const int tid = threadIdx.x;
-    uint32_t top = 0;
-    uint64_t count = 0;
+    using X = typename S::X;
+    uint32_t top_key = 0;
+    u64 count = 0;
     for (int k = 0; k < regions; ++k) {
-        top = parts[k].key > top ? parts[k].key : top;
+        top_key = parts[k].key > top_key ? parts[k].key : top_key;
         count += parts[k].count;
     }
     if (count == 0 || par.bad) {
-        if (tid == 0) write_nothing(a, r);
+        if (threadIdx.x == 0) write_nothing(a, r);
         return;
     }
+    const X top = S::value(top_key);
     if (par.T == 0.0f) {
         int first = 0;
-        while (parts[first].key != top) ++first;
-        const typename S::X best = S::value(top);
-        const int64_t found = pick_in_region<kLanes>(
-            row, Region(row.groups, regions, first), 0.5,
-            [&](typename S::X v, int64_t) { return v == best ? 1.0 : 0.0; }, sh);
-        if (tid == 0) {
-            a.pick[r] = (int32_t)found;
-            if (a.logp) a.logp[r] = 0.0f;
-            if (a.kept) a.kept[r] = 1;
-        }
+        while (parts[first].key != top_key) ++first;
+        pick_in_region<kLanes>(
+            row, Region(row.groups, regions, first), 0.5, Draw{a, r, (double)top, 0.0, 1.0, 1},
+            [&](const X (&v)[S::V], int, double (&w)[S::V]) {
+#pragma unroll
+                for (int e = 0; e < S::V; ++e) w[e] = v[e] == top ? 1.0 : 0.0;
+            },
+            sh);
         return;
     }
     Exponent ex;
-    ex.set(S::value(top), par.scale());
-    for (int k = tid; k < regions; k += kLanes)
+    ex.set(top, par.scale());
+    for (int k = threadIdx.x; k < regions; k += kLanes)
         scaled[k] = parts[k].count ? parts[k].weight * ex.weight(S::value(parts[k].key)) : 0.0;
     __syncthreads();
     double sum = 0.0;
@@ -378,48 +505,38 @@ __device__ void finish_row(const SampleArgs& a, int64_t r, const Row<S>& row, co
     }
     const double t = ((double)(a.rnd[r] >> 11) * 0x1p-53) * sum;
     double before = 0.0;
-    for (int k = 0; k < regions; ++k) {
+    for (int k = 0; k < target; ++k) {
         if (before + scaled[k] > t) {
             target = k;
             break;
         }
-        if (k == target) break;
         before += scaled[k];
     }
-    const int64_t found = pick_in_region<kLanes>(
-        row, Region(row.groups, regions, target), t - before,
-        [&](typename S::X v, int64_t) { return ex.weight(v); }, sh);
-    if (tid == 0) {
-        a.pick[r] = (int32_t)found;
-        if (a.logp) {
-            const double v = (double)S::widen(row.x[found]), m = (double)S::value(top);
-            const double z = v == m ? 0.0 : (v - m) / (double)par.T;
-            a.logp[r] = (float)(z - log(sum));
-        }
-        if (a.kept) a.kept[r] = (int32_t)count;
-    }
+    pick_in_region<kLanes>(
+        row, Region(row.groups, regions, target), t - before, Draw{a, r, (double)top, (double)par.T, sum, count},
+        [&](const X (&v)[S::V], int, double (&w)[S::V]) { ex.weights(v, w); }, sh);
 }
 
 // A row's split s of `splits`: workgroup r * splits + s.  With one split the row ends here.
 template <int kType>
 __global__ void __launch_bounds__(kAllLanes) all_kernel(SampleArgs a, int splits, Part* parts) {
     using S = Scores<kType>;
-    __shared__ Part own[kAllWaves];
-    __shared__ double scaled[kAllWaves];
+    constexpr int kRegions = kAllWaves * kAllRegions;
+    __shared__ Part own[kRegions];
+    __shared__ double scaled[kRegions];
     __shared__ PickShared<kAllLanes> sh;
     const int64_t r = a.row0 + blockIdx.x / splits;
-    const int s = blockIdx.x % splits, wave = threadIdx.x >> 6;
+    const int s = blockIdx.x % splits, wave = wave_index();
     const Row<S> row(a, r);
     const Parameters par(a, r);
-    const Part p = sum_region(row, Region(row.groups, splits * kAllWaves, s * kAllWaves + wave),
-                              par.T > 0.0f ? par.scale() : 0.0);
     if (splits > 1) {
-        if ((threadIdx.x & 63) == 0) parts[(r * splits + s) * kAllWaves + wave] = p;
+        sum_regions(row, splits * kAllWaves, s * kAllWaves + wave, 1, par, parts + (r * splits + s) * kAllWaves + wave);
         return;
     }
-    if ((threadIdx.x & 63) == 0) own[wave] = p;
+    const int each = a.N <= kShortRow ? 1 : kAllRegions;
+    sum_regions(row, kAllWaves * each, wave * each, each, par, own + wave * each);
     __syncthreads();
-    finish_row<kAllLanes>(a, r, row, par, own, kAllWaves, scaled, sh);
+    finish_row<kAllLanes>(a, r, row, par, own, kAllWaves * each, scaled, sh);
 }
 
 constexpr int kMaxSplits = 64;
@@ -439,131 +556,214 @@ __global__ void __launch_bounds__(kFinishLanes) finish_kernel(SampleArgs a, int 
 
 // ------------------------------------------------------------------ filters
 
-constexpr int kCutLanes = 1024, kCutWaves = kCutLanes / 64;
+constexpr int kCutLanes = 1024;
 constexpr int kBins = 2048;
-constexpr int kList = 512;
-
-struct CutShared {
-    uint32_t count[kBins];
-    u64 weight[kBins];
-    u64 list[kList];
-    u64 list_w[kList];
-    u64 wave_c[kCutWaves], wave_w[kCutWaves];
-    u64 above_c, above_w, total_w, found, found_w;
-    uint32_t bin, in_bin, listed, lo, hi;
-    Part part[kCutWaves];
-    PickShared<kCutLanes> pick;
-};
+constexpr int kList = 2048;
+constexpr int kRank = 64;
 
 // An entry's place in the order (descending score, ascending index): smaller is earlier.
-__device__ __forceinline__ u64 place_of(uint32_t key, int64_t index) {
-    return ((u64)~key << 32) | (u64)(uint32_t)index;
+__device__ __forceinline__ u64 place_of(uint32_t key, uint32_t index) { return ((u64)~key << 32) | index; }
+__device__ __forceinline__ uint32_t key_at(u64 place) { return ~(uint32_t)(place >> 32); }
+
+// The smallest key in (lo, hi] for which reached() holds (it holds for hi, and for every key above one for which it
+// does), by 64 probes a round; every lane of a wavefront calls it.
+template <class F>
+__device__ __forceinline__ uint32_t least_key(uint32_t lo, uint32_t hi, F reached) {
+    const int lane = threadIdx.x & 63;
+    while (hi - lo > 1) {
+        const uint32_t step = (hi - lo) / 65 + 1;
+        const u64 probe = (u64)lo + (u64)step * (lane + 1);
+        const u64 m = __ballot(probe >= hi || reached((uint32_t)probe));
+        const int first = m ? __ffsll(m) - 1 : 64;
+        const u64 up = (u64)lo + (u64)step * (first + 1);
+        lo += step * first;
+        hi = up < hi ? (uint32_t)up : hi;
+    }
+    return hi;
 }
 
-template <class S>
+template <int kLanes>
+struct CutShared {
+    static constexpr int kWaves = kLanes / 64;
+    uint32_t count[kBins];
+    u64 weight[kBins];
+    u64 list[kList], list_w[kList];
+    u64 some[kRank], some_w[kRank];
+    u64 wave_c[kWaves], wave_w[kWaves];
+    u64 above_c, above_w, in_bin, found, found_w, lo64, hi64;
+    uint32_t bin, listed, lo, hi;
+    Part part[kWaves];
+    PickShared<kLanes> pick;
+};
+
+// Where a row's filters end: the place of the last kept entry.
+template <int kLanes, class S>
 struct Cutter {
     using X = typename S::X;
+    static constexpr int kWaves = kLanes / 64, kOwn = kBins / kLanes;  // bins of a lane
     const Row<S>& row;
     Region mine;  // this wavefront's
     Exponent ex;
     X top;
-    float bins_per;  // level-0 bins per unit of score
-    double unit;     // whole-number weights are w * unit, rounded: sums below 2^62
+    uint32_t top_key;
+    float bins_per;  // distance bins per unit of score
+    int unit;        // whole-number weights are w 2^unit, rounded: the sums stay below 2^62
     bool weights;    // top-p is on
-    CutShared& sh;
+    bool filled;     // the bins hold the row's distances
+    CutShared<kLanes>& sh;
 
-    __device__ __forceinline__ u64 fixed(X v) const { return (u64)rint(ex.weight(v) * unit); }
+    // w 2^unit, rounded, is what adding 2^(52 - unit) leaves in the low bits (unit <= 51, w <= 1).
+    __device__ __forceinline__ u64 fixed(double w) const {
+        const double one = __longlong_as_double((long long)(1075 - unit) << 52);
+        return (u64)__double_as_longlong(w + one) - (u64)__double_as_longlong(one);
+    }
+    __device__ __forceinline__ u64 fixed_of(X v) const { return weights ? fixed(ex.weight(v)) : 0; }
     // Distance bins: equal scores share one, and a lower score is never in an earlier one.  NaN (inf - inf, or the
     // top itself where bins_per is infinite) goes to the first bin, what is past the range to the last.
     __device__ __forceinline__ uint32_t bin_of(X v) const {
         const float b = S::below(top, v) * bins_per;
         return b >= (float)(kBins - 1) ? kBins - 1 : b > 0.0f ? (uint32_t)b : 0u;
     }
-    // body(v, index) for every entry of this wavefront's region that is not masked.
     template <class B>
     __device__ __forceinline__ void walk(B body) const {
-        const int lane = threadIdx.x & 63;
-        for (int64_t g = mine.lo + lane; g < mine.hi; g += 64) {
-            X v[S::V];
-            row.load(g, v);
-            const int64_t i = row.first(g);
-#pragma unroll
-            for (int e = 0; e < S::V; ++e)
-                if (v[e] != S::kMasked) body(v[e], i + e);
-        }
+        row.walk(mine.lo, mine.hi, body);
     }
 
-    __device__ void clear_bins() {
-        for (int b = threadIdx.x; b < kBins; b += kCutLanes) {
-            sh.count[b] = 0;
-            sh.weight[b] = 0;
+    __device__ __forceinline__ void clear_bins() {
+#pragma unroll
+        for (int i = 0; i < kOwn; ++i) {
+            sh.count[threadIdx.x + i * kLanes] = 0;
+            sh.weight[threadIdx.x + i * kLanes] = 0;
         }
+        filled = false;
         __syncthreads();
     }
 
-    // The bin, from 0 up, in which the count passes want or the weight reaches goal; above_c and above_w of the
-    // earlier ones are added to those of the call.
-    template <bool kByWeight>
-    __device__ void cross(u64 want, double goal, u64 above_c, u64 above_w) {
-        const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
-        const u64 c0 = sh.count[2 * tid], c1 = sh.count[2 * tid + 1];
-        const u64 w0 = sh.weight[2 * tid], w1 = sh.weight[2 * tid + 1];
-        const u64 sc = wave_scan(c0 + c1), sw = wave_scan(w0 + w1);
+    // Counts (of every entry, masked ones last) and weights by distance bin.  The last bin's are summed in registers:
+    // most entries can be there.
+    __device__ void fill_bins(bool counts) {
+        clear_bins();
+        const int lane = threadIdx.x & 63;
+        uint32_t far = 0;
+        u64 far_w = 0;
+        if (weights) {
+            walk([&](const X (&v)[S::V], int) {
+                double w[S::V];
+                ex.weights(v, w);
+#pragma unroll
+                for (int e = 0; e < S::V; ++e) {
+                    const uint32_t b = bin_of(v[e]);
+                    if (b == kBins - 1) {
+                        far_w += fixed(w[e]);
+                        ++far;
+                    } else {
+                        atomicAdd(&sh.weight[b], fixed(w[e]));
+                        if (counts) atomicAdd(&sh.count[b], 1u);
+                    }
+                }
+            });
+        } else {
+            walk([&](const X (&v)[S::V], int) {
+#pragma unroll
+                for (int e = 0; e < S::V; ++e) {
+                    const uint32_t b = bin_of(v[e]);
+                    if (b == kBins - 1) ++far;
+                    else atomicAdd(&sh.count[b], 1u);
+                }
+            });
+        }
+        for (int o = 32; o > 0; o >>= 1) {
+            far += (uint32_t)__shfl_xor((int)far, o, 64);
+            far_w += __shfl_xor(far_w, o, 64);
+        }
+        if (lane == 0) {
+            atomicAdd(&sh.count[kBins - 1], far);
+            atomicAdd(&sh.weight[kBins - 1], far_w);
+        }
+        filled = true;
+        __syncthreads();
+    }
+
+    __device__ u64 total_weight() {
+        u64 w = 0;
+#pragma unroll
+        for (int i = 0; i < kOwn; ++i) w += sh.weight[threadIdx.x + i * kLanes];
+        for (int o = 32; o > 0; o >>= 1) w += __shfl_xor(w, o, 64);
+        if ((threadIdx.x & 63) == 0) sh.wave_w[wave_index()] = w;
+        __syncthreads();
+        w = 0;
+        for (int k = 0; k < kWaves; ++k) w += sh.wave_w[k];
+        __syncthreads();
+        return w;
+    }
+
+    // The bin, from 0 up, in which the count passes want or the weight reaches goal; above_c and above_w are those of
+    // what precedes the bins.  Leaves bin, in_bin, above_c and above_w in LDS.
+    __device__ void cross(bool by_weight, u64 want, double goal, u64 above_c, u64 above_w) {
+        const int wave = wave_index(), lane = threadIdx.x & 63;
+        u64 c[kOwn], w[kOwn], sum_c = 0, sum_w = 0;
+#pragma unroll
+        for (int i = 0; i < kOwn; ++i) {
+            c[i] = sh.count[kOwn * threadIdx.x + i];
+            w[i] = weights ? sh.weight[kOwn * threadIdx.x + i] : 0;
+            sum_c += c[i];
+            sum_w += w[i];
+        }
+        const u64 sc = wave_scan(sum_c), sw = weights ? wave_scan(sum_w) : 0;
         if (lane == 63) {
             sh.wave_c[wave] = sc;
             sh.wave_w[wave] = sw;
         }
         __syncthreads();
-        u64 ec = above_c + sc - (c0 + c1), ew = above_w + sw - (w0 + w1);
+        u64 ec = above_c + sc - sum_c, ew = above_w + sw - sum_w;
         for (int k = 0; k < wave; ++k) {
             ec += sh.wave_c[k];
             ew += sh.wave_w[k];
         }
 #pragma unroll
-        for (int q = 0; q < 2; ++q) {
-            const u64 c = q ? c1 : c0, w = q ? w1 : w0;
-            const bool here = kByWeight ? (double)ew < goal && (double)(ew + w) >= goal : ec < want && ec + c >= want;
+        for (int i = 0; i < kOwn; ++i) {
+            const bool here = by_weight ? (double)ew < goal && (double)(ew + w[i]) >= goal
+                                        : ec < want && ec + c[i] >= want;
             if (here) {
-                sh.bin = 2 * tid + q;
-                sh.in_bin = (uint32_t)c;
+                sh.bin = kOwn * threadIdx.x + i;
+                sh.in_bin = c[i];
                 sh.above_c = ec;
                 sh.above_w = ew;
             }
-            ec += c;
-            ew += w;
+            ec += c[i];
+            ew += w[i];
         }
         __syncthreads();
     }
 
-    // Index place of the number-th entry (from 1) whose score is v, in index order.
+    // Place of the number-th entry (from 1) whose score is v, in index order.
     __device__ u64 nth_equal(X v, u64 number) {
-        const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
-        uint32_t n = 0;
-        walk([&](X x, int64_t) { n += x == v; });
-        const uint32_t in_region = wave_sum(n);
-        if (lane == 0) sh.wave_c[wave] = in_region;
+        const int wave = wave_index(), lane = threadIdx.x & 63;
+        u64 n = 0;
+        walk([&](const X (&x)[S::V], int) {
+#pragma unroll
+            for (int e = 0; e < S::V; ++e) n += __popcll(__ballot(x[e] == v));
+        });
+        if (lane == 0) sh.wave_c[wave] = n;
         __syncthreads();
         u64 before = 0;
         for (int k = 0; k < wave; ++k) before += sh.wave_c[k];
-        if (before < number && before + in_region >= number) {
+        if (before < number && before + n >= number) {
             u64 seen = before;
-            for (int64_t g0 = mine.lo; g0 < mine.hi; g0 += 64) {
-                X x[S::V];
+            walk([&](const X (&x)[S::V], int first) {
+                if (seen >= number) return;
                 uint32_t here = 0;
-                if (g0 + lane < mine.hi) {
-                    row.load(g0 + lane, x);
 #pragma unroll
-                    for (int e = 0; e < S::V; ++e) here += x[e] == v;
-                }
+                for (int e = 0; e < S::V; ++e) here += x[e] == v;
                 const uint32_t scan = wave_scan(here);
                 u64 at = seen + scan - here;
-                if (here > 0 && at < number && at + here >= number) {
+                if (at < number && at + here >= number) {
+#pragma unroll
                     for (int e = 0; e < S::V; ++e)
-                        if (x[e] == v && ++at == number) sh.found = place_of(S::key(v), row.first(g0 + lane) + e);
+                        if (x[e] == v && ++at == number) sh.found = place_of(S::key(v), (uint32_t)(first + e));
                 }
                 seen += (uint32_t)__shfl((int)scan, 63, 64);
-                if (seen >= number) break;
-            }
+            });
         }
         __syncthreads();
         const u64 r = sh.found;
@@ -571,16 +771,95 @@ struct Cutter {
         return r;
     }
 
-    // The entry at which the count reaches want (kByWeight false) or the weight reaches goal, in the order; the
-    // level-0 bins hold their sums.  *up_to: the weight up to and with it (where weights are summed).
-    template <bool kByWeight>
-    __device__ u64 cut(u64 want, double goal, u64* up_to) {
+    // The cut among the listed entries: split by the bits of their places until at most kRank are left, which a
+    // wavefront ranks.
+    __device__ u64 cut_list(uint32_t number, bool by_weight, u64 want, double goal, u64 above_c, u64 above_w, u64* up_to) {
         const int tid = threadIdx.x;
-        cross<kByWeight>(want, goal, 0, 0);
-        bool level0 = true;
-        uint32_t lo = 0, hi = 0;  // keys of the bin, after level 0
+        u64 lo = 0, hi = ~(u64)0;  // places still in question
+        if (tid == 0) sh.in_bin = number;
+        __syncthreads();
+        while (sh.in_bin > kRank) {
+            if (tid == 0) {
+                sh.lo64 = ~(u64)0;
+                sh.hi64 = 0;
+            }
+            clear_bins();
+            u64 least = ~(u64)0, most = 0;
+            for (uint32_t i = tid; i < number; i += kLanes) {
+                const u64 p = sh.list[i];
+                if (p < lo || p > hi) continue;
+                least = p < least ? p : least;
+                most = p > most ? p : most;
+            }
+            least = ~wave_max(~least);
+            most = wave_max(most);
+            if ((tid & 63) == 0 && most >= least) {
+                atomicMin(&sh.lo64, least);
+                atomicMax(&sh.hi64, most);
+            }
+            __syncthreads();
+            lo = sh.lo64;
+            hi = sh.hi64;
+            const u64 spread = (hi - lo) >> 11;
+            const int shift = spread ? 64 - __clzll(spread) : 0;
+            for (uint32_t i = tid; i < number; i += kLanes) {
+                const u64 p = sh.list[i];
+                if (p < lo || p > hi) continue;
+                const uint32_t b = (uint32_t)((p - lo) >> shift);
+                atomicAdd(&sh.count[b], 1u);
+                if (weights) atomicAdd(&sh.weight[b], sh.list_w[i]);
+            }
+            __syncthreads();
+            cross(by_weight, want, goal, above_c, above_w);
+            above_c = sh.above_c;
+            above_w = sh.above_w;
+            lo += (u64)sh.bin << shift;
+            const u64 end = lo + (((u64)1 << shift) - 1);
+            hi = end < hi ? end : hi;
+        }
+        // at most kRank entries: one wavefront's lanes, each against all
+        if (tid == 0) sh.listed = 0;
+        __syncthreads();
+        for (uint32_t i = tid; i < number; i += kLanes) {
+            const u64 p = sh.list[i];
+            if (p < lo || p > hi) continue;
+            const uint32_t at = atomicAdd(&sh.listed, 1u);
+            sh.some[at] = p;
+            sh.some_w[at] = sh.list_w[i];
+        }
+        __syncthreads();
+        const uint32_t left = sh.listed;
+        if ((uint32_t)tid < left) {
+            const u64 p = sh.some[tid], w = sh.some_w[tid];
+            u64 before = above_c, before_w = above_w;
+            for (uint32_t j = 0; j < left; ++j) {
+                const bool earlier = sh.some[j] < p;
+                before += earlier;
+                before_w += earlier ? sh.some_w[j] : 0;
+            }
+            if (by_weight ? (double)before_w < goal && (double)(before_w + w) >= goal : before + 1 == want) {
+                sh.found = p;
+                sh.found_w = before_w + w;
+            }
+        }
+        __syncthreads();
+        const u64 r = sh.found;
+        *up_to = sh.found_w;
+        __syncthreads();
+        return r;
+    }
+
+    // The entry at which the count reaches want (by_weight false) or the weight reaches goal, in the order; the
+    // distance bins hold their sums.  *up_to: the weight up to and with it (where weights are summed).
+    __device__ u64 cut(bool by_weight, u64 want, double goal, u64* up_to) {
+        const int tid = threadIdx.x;
+        cross(by_weight, want, goal, 0, 0);
+        // the bin's keys: from the smallest that is in it or an earlier one to the last before the earlier ones
+        const uint32_t bin = sh.bin, none = S::key(S::kMasked);
+        uint32_t lo = least_key(none, top_key, [&](uint32_t k) { return bin_of(S::value(k)) <= bin; });
+        uint32_t hi = bin == 0 ? top_key
+                               : least_key(none, top_key, [&](uint32_t k) { return bin_of(S::value(k)) < bin; }) - 1;
         for (;;) {
-            const uint32_t bin = sh.bin;
             const u64 above_c = sh.above_c, above_w = sh.above_w;
             __syncthreads();
             if (tid == 0) {
@@ -589,60 +868,40 @@ struct Cutter {
                 sh.hi = 0;
             }
             __syncthreads();
-            // the bin's entries into the list, and their range of keys
-            uint32_t least = 0xFFFFFFFFu, most = 0;
-            walk([&](X v, int64_t i) {
-                const uint32_t k = S::key(v);
-                if (level0 ? bin_of(v) != bin : k < lo || k > hi) return;
-                least = k < least ? k : least;
-                most = k > most ? k : most;
-                const uint32_t at = atomicAdd(&sh.listed, 1u);
-                if (at < kList) sh.list[at] = place_of(k, i);
+            // the entries with these keys into the list, and the range they take
+            const X from = S::value(lo), to = S::value_up(hi);
+            X least = to, most = from;
+            uint32_t any = 0;
+            walk([&](const X (&v)[S::V], int first) {
+#pragma unroll
+                for (int e = 0; e < S::V; ++e) {
+                    if (v[e] >= from && v[e] <= to) {
+                        least = v[e] < least ? v[e] : least;
+                        most = v[e] > most ? v[e] : most;
+                        any = 1;
+                        const uint32_t at = atomicAdd(&sh.listed, 1u);
+                        if (at < kList) sh.list[at] = place_of(S::key(v[e]), (uint32_t)(first + e));
+                    }
+                }
             });
-            if (most >= least) {
-                atomicMin(&sh.lo, least);
-                atomicMax(&sh.hi, most);
+            if (any) {
+                atomicMin(&sh.lo, S::key(least));
+                atomicMax(&sh.hi, S::key(most));
             }
             __syncthreads();
-            level0 = false;
             lo = sh.lo;
             hi = sh.hi;
             const uint32_t number = sh.listed;
             if (number <= kList) {
-                // each lane's entry against all: how many come before it, and their weight
-                u64 mine_at = 0, w = 0;
-                if (tid < (int)number) {
-                    mine_at = sh.list[tid];
-                    w = weights ? fixed(S::value(~(uint32_t)(mine_at >> 32))) : 0;
-                    sh.list_w[tid] = w;
-                }
-                __syncthreads();
-                if (tid < (int)number) {
-                    u64 before = 0, before_w = above_w;
-                    for (uint32_t j = 0; j < number; ++j) {
-                        const bool earlier = sh.list[j] < mine_at;
-                        before += earlier;
-                        before_w += earlier ? sh.list_w[j] : 0;
-                    }
-                    const bool here = kByWeight ? (double)before_w < goal && (double)(before_w + w) >= goal
-                                                : above_c + before + 1 == want;
-                    if (here) {
-                        sh.found = mine_at;
-                        sh.found_w = before_w + w;
-                    }
-                }
-                __syncthreads();
-                const u64 r = sh.found;
-                *up_to = sh.found_w;
-                __syncthreads();
-                return r;
+                for (uint32_t i = tid; i < number; i += kLanes) sh.list_w[i] = fixed_of(S::value(key_at(sh.list[i])));
+                return cut_list(number, by_weight, want, goal, above_c, above_w, up_to);
             }
             if (lo == hi) {  // equal scores: as many of them as it takes, in index order
                 const X v = S::value(lo);
-                const u64 w = weights ? fixed(v) : 0;
+                const u64 w = fixed_of(v);
                 u64 r;
-                if (kByWeight) {
-                    const double q = (goal - (double)above_w) / (double)w;  // w > 0: the weight passes goal in this bin
+                if (by_weight) {
+                    const double q = (goal - (double)above_w) / (double)w;  // w > 0: the weight reaches goal here
                     r = q < 1.0 ? 1 : q >= (double)number ? number : (u64)q;
                     while (r > 1 && (double)(above_w + (r - 1) * w) >= goal) --r;
                     while (r < number && (double)(above_w + r * w) < goal) ++r;
@@ -655,96 +914,121 @@ struct Cutter {
             // split the range of keys: 2,048 bins from the largest key down
             const int shift = 32 - __clz((hi - lo) >> 11);
             clear_bins();
-            walk([&](X v, int64_t) {
-                const uint32_t k = S::key(v);
-                if (k < lo || k > hi) return;
-                const uint32_t b = (hi - k) >> shift;
-                atomicAdd(&sh.count[b], 1u);
-                if (weights) atomicAdd(&sh.weight[b], fixed(v));
+            walk([&](const X (&v)[S::V], int) {
+#pragma unroll
+                for (int e = 0; e < S::V; ++e) {
+                    const uint32_t k = S::key(v[e]);
+                    if (k < lo || k > hi) continue;
+                    const uint32_t b = (hi - k) >> shift;
+                    atomicAdd(&sh.count[b], 1u);
+                    if (weights) atomicAdd(&sh.weight[b], fixed_of(v[e]));
+                }
             });
             __syncthreads();
-            cross<kByWeight>(want, goal, above_c, above_w);
-            const uint32_t b = sh.bin;
-            const uint32_t top_key = hi - (b << shift);
-            const uint32_t span = (1u << shift) - 1;
-            lo = top_key - lo > span ? top_key - span : lo;
-            hi = top_key;
+            cross(by_weight, want, goal, above_c, above_w);
+            const uint32_t b = sh.bin, span = (1u << shift) - 1;
+            hi -= b << shift;
+            lo = hi - lo > span ? hi - span : lo;
         }
     }
-    __device__ void fill_bins(bool counts) {
-        clear_bins();
-        walk([&](X v, int64_t) {
-            const uint32_t b = bin_of(v);
-            if (counts) atomicAdd(&sh.count[b], 1u);
-            if (weights) atomicAdd(&sh.weight[b], fixed(v));
-        });
-        __syncthreads();
-    }
-    __device__ u64 total_weight() {
-        const int wave = threadIdx.x >> 6;
-        u64 w = sh.weight[2 * threadIdx.x] + sh.weight[2 * threadIdx.x + 1];
-        w = wave_scan(w);
-        if ((threadIdx.x & 63) == 63) sh.wave_w[wave] = w;
-        __syncthreads();
-        w = 0;
-        for (int k = 0; k < kCutWaves; ++k) w += sh.wave_w[k];
-        __syncthreads();
-        return w;
+
+    // The last kept place by all filters.
+    __device__ u64 last_kept(const Parameters& par, uint32_t eligible) {
+        if (par.T == 0.0f || par.q > 1.0f || par.p <= 0.0f) return nth_equal(top, 1);  // one entry is kept always
+        const bool by_k = par.k > 0 && (uint32_t)par.k < eligible, by_p = par.p < 1.0f;
+        u64 last = ~(u64)0;
+        weights = by_p;
+        u64 total = 0;
+#pragma unroll 1
+        for (int by_weight = by_k ? 0 : 1; by_weight <= (by_p ? 1 : 0); ++by_weight) {
+            // top-k's cut first: top-p goes by the weight of the first k, and reaches its share of that before the last
+            // of them
+            if (!filled) fill_bins(by_k && !by_weight);
+            if (by_weight && !by_k) total = total_weight();
+            u64 up_to = 0;
+            const u64 at = cut(by_weight != 0, (u64)par.k, (double)par.p * (double)total, &up_to);
+            last = at < last ? at : last;
+            total = up_to;
+        }
+        if (par.q > 0.0f) {
+            const uint32_t k = least_key(S::key(S::kMasked), top_key,
+                                         [&](uint32_t p) { return ex.weight(S::value(p)) >= (double)par.q; });
+            const u64 at = place_of(k, 0xFFFFFFFFu);
+            last = at < last ? at : last;
+        }
+        return last;
     }
 };
 
-// The smallest key whose weight is at least q, by 64 probes a round; every lane of a wavefront calls it.
+// Whether an entry is kept: everything up to a place.
 template <class S>
-__device__ uint32_t key_of_weight(const Exponent& ex, typename S::X top, double q) {
-    const int lane = threadIdx.x & 63;
-    uint32_t lo = S::key(S::kMasked), hi = S::key(top);  // weight(lo) < q <= weight(hi)
-    while (hi - lo > 1) {
-        const uint32_t step = (hi - lo) / 65 + 1;
-        const u64 probe = (u64)lo + (u64)step * (lane + 1);
-        const bool reached = probe >= hi || ex.weight(S::value((uint32_t)probe)) >= q;
-        const u64 m = __ballot(reached);  // never 0 in the last lane: lo + 64 step >= hi - step
-        const int first = m ? __ffsll(m) - 1 : 64;
-        const u64 up = (u64)lo + (u64)step * (first + 1);
-        lo += step * first;
-        hi = up < hi ? (uint32_t)up : hi;
+struct Kept {
+    using X = typename S::X;
+    X edge;
+    int edge_at;
+    __device__ __forceinline__ explicit Kept(u64 last) {
+        edge = last == ~(u64)0 ? S::kMasked : S::value(key_at(last));
+        edge_at = (uint32_t)last > 0x7FFFFFFFu ? INT32_MAX : (int)(uint32_t)last;
     }
-    return hi;
-}
+    __device__ __forceinline__ bool operator()(X v, int i) const {
+        return v > edge || (v == edge && i <= edge_at && v != S::kMasked);
+    }
+    // Weights of a lane's entries, 0 for those not kept; skipped where no lane of the wavefront keeps one.
+    __device__ __forceinline__ bool weights(const Exponent& ex, bool greedy, const X (&v)[S::V], int first,
+                                            double (&w)[S::V], uint32_t* count) const {
+        bool keep[S::V], some = false;
+#pragma unroll
+        for (int e = 0; e < S::V; ++e) {
+            keep[e] = (*this)(v[e], first + e);
+            some = some || keep[e];
+        }
+#pragma unroll
+        for (int e = 0; e < S::V; ++e) w[e] = 0.0;
+        if (!__any(some)) return false;
+        if (!greedy) ex.weights(v, w);
+#pragma unroll
+        for (int e = 0; e < S::V; ++e) {
+            w[e] = !keep[e] ? 0.0 : greedy ? 1.0 : w[e];
+            *count += __popcll(__ballot(keep[e]));
+        }
+        return true;
+    }
+};
 
 template <int kType>
 __global__ void __launch_bounds__(kCutLanes) cut_kernel(SampleArgs a) {
     using S = Scores<kType>;
     using X = typename S::X;
-    __shared__ CutShared sh;
-    const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
+    constexpr int kWaves = kCutLanes / 64;
+    __shared__ CutShared<kCutLanes> sh;
+    const int tid = threadIdx.x, wave = wave_index(), lane = tid & 63;
     const int64_t r = a.row0 + blockIdx.x;
     const Row<S> row(a, r);
     const Parameters par(a, r);
-    const Region mine(row.groups, kCutWaves, wave);
+    const Region mine(row.groups, kWaves, wave);
 
     // the largest score, the smallest one, the number of entries
-    X top = S::kMasked, low = S::value(0xFFFFFFFFu - (kType == HX_SCORE_I32 ? 0u : 0x7FFFFFu));
+    X most = S::kMasked, least = S::value(0xFFFFFFFFu - (kType == HX_SCORE_I32 ? 0u : 0x7FFFFFu));
     uint32_t eligible = 0;
-    for (int64_t g = mine.lo + lane; g < mine.hi; g += 64) {
-        X v[S::V];
-        row.load(g, v);
+    row.walk(mine.lo, mine.hi, [&](const X (&v)[S::V], int) {
 #pragma unroll
         for (int e = 0; e < S::V; ++e) {
-            top = v[e] > top ? v[e] : top;
-            low = v[e] != S::kMasked && v[e] < low ? v[e] : low;
-            eligible += v[e] != S::kMasked;
+            most = S::larger(most, v[e]);
+            least = v[e] != S::kMasked && v[e] < least ? v[e] : least;
+            eligible += __popcll(__ballot(v[e] != S::kMasked));
         }
+    });
+    if (tid == 0) {
+        sh.listed = sh.hi = 0;
+        sh.lo = 0xFFFFFFFFu;
     }
-    if (tid == 0) sh.listed = sh.hi = 0;
-    if (tid == 0) sh.lo = 0xFFFFFFFFu;
     __syncthreads();
-    eligible = wave_sum(eligible);
     if (eligible) {
-        const uint32_t most = wave_max(S::key(top)), least = ~wave_max(~S::key(low));
+        const uint32_t up = wave_max(S::key(most)), down = ~wave_max(~S::key(least));
         if (lane == 0) {
             atomicAdd(&sh.listed, eligible);
-            atomicMax(&sh.hi, most);
-            atomicMin(&sh.lo, least);
+            atomicMax(&sh.hi, up);
+            atomicMin(&sh.lo, down);
         }
     }
     __syncthreads();
@@ -753,77 +1037,44 @@ __global__ void __launch_bounds__(kCutLanes) cut_kernel(SampleArgs a) {
         if (tid == 0) write_nothing(a, r);
         return;
     }
-    top = S::value(sh.hi);
-    low = S::value(sh.lo);
+    const uint32_t top_key = sh.hi;
+    const X top = S::value(top_key), low = S::value(sh.lo);
     __syncthreads();
 
     const bool greedy = par.T == 0.0f;
-    // weights past 24 T below the top add less than 4e-11 each: their bins need no width of their own
+    // weights past 24 T below the top add less than 4e-11 each: their bins need no width of their own; a count alone
+    // goes by the scores' range
     const float reach = 24.0f * par.T, spread = S::below(top, low);
     Exponent ex;
     ex.set(top, greedy ? 0.0 : par.scale());
-    Cutter<S> cut{row, mine, ex, top, (float)(kBins - 1) / (reach < spread ? reach : spread), 0.0, false, sh};
-    u64 last = ~(u64)0;  // place of the last kept entry
-    if (greedy || par.q > 1.0f || par.p <= 0.0f) {
-        last = cut.nth_equal(top, 1);  // one entry is kept always
-    } else {
-        const bool by_k = par.k > 0 && (uint32_t)par.k < eligible, by_p = par.p < 1.0f;
-        cut.weights = by_p;
-        cut.unit = ldexp(1.0, 62 - (row.n > 1 ? 32 - __clz(row.n - 1) : 0));
-        if (by_k || by_p) {
-            cut.fill_bins(by_k);
-            u64 total = by_p ? cut.total_weight() : 0, up_to = 0;
-            if (by_k) {
-                last = cut.template cut<false>((u64)par.k, 0.0, &up_to);
-                total = up_to;
-            }
-            if (by_p) {
-                // within the first k: their weight reaches p of itself before the last of them does
-                if (by_k) cut.fill_bins(true);
-                const u64 at = cut.template cut<true>(0, (double)par.p * (double)total, &up_to);
-                last = at < last ? at : last;
-            }
-        }
-        if (par.q > 0.0f) {
-            const u64 at = place_of(key_of_weight<S>(ex, top, (double)par.q), 0xFFFFFFFFll);
-            last = at < last ? at : last;
-        }
-    }
+    Cutter<kCutLanes, S> cut{row, mine, ex, top, top_key,
+                             (float)(kBins - 1) / (par.p < 1.0f && reach < spread ? reach : spread), 0, false,
+                             false, sh};
+    const int bits = row.n > 1 ? 32 - __clz(row.n - 1) : 0;
+    cut.unit = bits < 11 ? 51 : 62 - bits;
+    const Kept<S> kept(cut.last_kept(par, eligible));
 
     // weight and number of the kept entries, by region
-    const bool all = last == ~(u64)0;
-    const X edge = all ? S::kMasked : S::value(~(uint32_t)(last >> 32));
-    const int64_t edge_at = (int64_t)(uint32_t)last;
-    const auto weight = [&](X v, int64_t i) {
-        const bool kept = v != S::kMasked && (v > edge || (v == edge && i <= edge_at));
-        return !kept ? 0.0 : greedy ? 1.0 : ex.weight(v);
-    };
     double sum = 0.0;
     uint32_t number = 0;
-    for (int64_t g = mine.lo + lane; g < mine.hi; g += 64) {
-        X v[S::V];
-        row.load(g, v);
-        const int64_t i = row.first(g);
+    row.walk(mine.lo, mine.hi, [&](const X (&v)[S::V], int first) {
+        double w[S::V];
+        if (!kept.weights(ex, greedy, v, first, w, &number)) return;
 #pragma unroll
-        for (int e = 0; e < S::V; ++e) {
-            if (v[e] == S::kMasked || v[e] < edge || (v[e] == edge && i + e > edge_at)) continue;
-            sum += greedy ? 1.0 : ex.weight(v[e]);
-            ++number;
-        }
-    }
+        for (int e = 0; e < S::V; ++e) sum += w[e];
+    });
     sum = wave_sum(sum);
-    number = wave_sum(number);
     if (lane == 0) sh.part[wave] = Part{sum, 0u, number};
     __syncthreads();
-    double S_all = 0.0;
-    u64 kept = 0;
+    double all = 0.0;
+    u64 count = 0;
     int target = 0;
-    for (int k = 0; k < kCutWaves; ++k) {
-        S_all += sh.part[k].weight;
-        kept += sh.part[k].count;
+    for (int k = 0; k < kWaves; ++k) {
+        all += sh.part[k].weight;
+        count += sh.part[k].count;
         if (sh.part[k].weight > 0.0) target = k;
     }
-    const double t = ((double)(a.rnd[r] >> 11) * 0x1p-53) * S_all;
+    const double t = ((double)(a.rnd[r] >> 11) * 0x1p-53) * all;
     double before = 0.0;
     for (int k = 0; k < target; ++k) {
         if (before + sh.part[k].weight > t) {
@@ -832,16 +1083,13 @@ __global__ void __launch_bounds__(kCutLanes) cut_kernel(SampleArgs a) {
         }
         before += sh.part[k].weight;
     }
-    const int64_t found = pick_in_region<kCutLanes>(row, Region(row.groups, kCutWaves, target), t - before, weight, sh.pick);
-    if (tid == 0) {
-        a.pick[r] = (int32_t)found;
-        if (a.logp) {
-            const double v = (double)S::widen(row.x[found]), m = (double)top;
-            const double z = v == m ? 0.0 : (v - m) / (double)par.T;
-            a.logp[r] = greedy ? 0.0f : (float)(z - log(S_all));
-        }
-        if (a.kept) a.kept[r] = (int32_t)kept;
-    }
+    pick_in_region<kCutLanes>(
+        row, Region(row.groups, kWaves, target), t - before, Draw{a, r, (double)top, (double)par.T, all, count},
+        [&](const X (&v)[S::V], int first, double (&w)[S::V]) {
+            uint32_t n = 0;
+            kept.weights(ex, greedy, v, first, w, &n);
+        },
+        sh.pick);
 }
 
 // Workgroups a row without filters is split into: until the chip has two for every CU, with 4,096 entries
