@@ -272,25 +272,54 @@ __device__ __forceinline__ void write_nothing(const SampleArgs& a, int64_t r) {
 
 // ------------------------------------------------------------------ wavefront sums
 
-__device__ __forceinline__ double wave_sum(double v) {
-    for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o, 64);
-    return v;
+// Sums and maxima over the lanes by data-parallel moves (rows of 16 lanes shifted by 1, 2, 4 and 8, then the rows'
+// last lanes broadcast on), which take a tenth of the time of moves through LDS.  A lane without a source gets `idle`.
+template <int kControl, int kRows, class A>
+__device__ __forceinline__ A move(A v, A idle) {
+    static_assert(sizeof(A) == 4 || sizeof(A) == 8, "whole registers");
+    int from[sizeof(A) / 4], none[sizeof(A) / 4], to[sizeof(A) / 4];
+    __builtin_memcpy(from, &v, sizeof(A));
+    __builtin_memcpy(none, &idle, sizeof(A));
+#pragma unroll
+    for (int k = 0; k < (int)sizeof(A) / 4; ++k)
+        to[k] = __builtin_amdgcn_update_dpp(none[k], from[k], kControl, kRows, 0xf, false);
+    A r;
+    __builtin_memcpy(&r, to, sizeof(A));
+    return r;
 }
-template <class X>
-__device__ __forceinline__ X wave_max(X v) {
-    for (int o = 32; o > 0; o >>= 1) {
-        const X p = __shfl_xor(v, o, 64);
-        v = p > v ? p : v;
-    }
+template <class A>
+__device__ __forceinline__ A last_lane(A v) {
+    int w[sizeof(A) / 4];
+    __builtin_memcpy(w, &v, sizeof(A));
+#pragma unroll
+    for (int k = 0; k < (int)sizeof(A) / 4; ++k) w[k] = __builtin_amdgcn_readlane(w[k], 63);
+    __builtin_memcpy(&v, w, sizeof(A));
     return v;
 }
 template <class A>
 __device__ __forceinline__ A wave_scan(A v) {  // inclusive
-    for (int o = 1; o < 64; o <<= 1) {
-        const A p = __shfl_up(v, o, 64);
-        if ((int)(threadIdx.x & 63) >= o) v += p;
-    }
+    v += move<0x111, 0xf>(v, A(0));
+    v += move<0x112, 0xf>(v, A(0));
+    v += move<0x114, 0xf>(v, A(0));
+    v += move<0x118, 0xf>(v, A(0));
+    v += move<0x142, 0xa>(v, A(0));
+    v += move<0x143, 0xc>(v, A(0));
     return v;
+}
+template <class A>
+__device__ __forceinline__ A wave_sum(A v) {
+    return last_lane(wave_scan(v));
+}
+template <class A>
+__device__ __forceinline__ A wave_max(A v) {
+    const auto larger = [](A a, A b) { return b > a ? b : a; };
+    v = larger(v, move<0x111, 0xf>(v, v));
+    v = larger(v, move<0x112, 0xf>(v, v));
+    v = larger(v, move<0x114, 0xf>(v, v));
+    v = larger(v, move<0x118, 0xf>(v, v));
+    v = larger(v, move<0x142, 0xa>(v, v));
+    v = larger(v, move<0x143, 0xc>(v, v));
+    return last_lane(v);
 }
 
 // ------------------------------------------------------------------ the draw
@@ -318,7 +347,43 @@ template <int kLanes>
 struct PickShared {
     double wave[kLanes / 64];
     int found[kLanes / 64], last[kLanes / 64];
+    double before;
+    int target;
 };
+
+// The region in which the draw u falls, given each lane's region's weight (lanes in index order, at most one region a
+// lane, some weight above 0): the weight of all to *sum, of the regions before it to *before.  one: the first region
+// with weight.
+template <int kLanes>
+__device__ int target_region(double mine, double u, bool one, double* sum, double* before, PickShared<kLanes>& sh) {
+    constexpr int kWaves = kLanes / 64;
+    const int wave = wave_index(), lane = threadIdx.x & 63;
+    const double scan = wave_scan(mine);
+    const u64 has = __ballot(mine > 0.0);
+    if (lane == 63) {
+        sh.wave[wave] = scan;
+        sh.last[wave] = has ? wave * 64 + 63 - __clzll(has) : -1;
+    }
+    __syncthreads();
+    double ahead = 0.0, all = 0.0;
+    int last = 0;
+    for (int k = 0; k < kWaves; ++k) {
+        if (k == wave) ahead = all;
+        all += sh.wave[k];
+        last = sh.last[k] >= 0 ? sh.last[k] : last;
+    }
+    const double t = one ? 0.0 : u * all;
+    const u64 past = __ballot(mine > 0.0 && ahead + scan > t);
+    if (lane == 0) sh.found[wave] = past ? wave * 64 + __ffsll(past) - 1 : kLanes;
+    __syncthreads();
+    int target = last;  // where rounding leaves t unreached
+    for (int k = kWaves - 1; k >= 0; --k) target = sh.found[k] < kLanes ? sh.found[k] : target;
+    if ((int)threadIdx.x == target) sh.before = ahead + (scan - mine);
+    __syncthreads();
+    *sum = all;
+    *before = sh.before;
+    return target;
+}
 
 // The first entry of groups [lo, hi) up to which the weights sum to more than t, or the last one with weight
 // (which rounding can leave as the only choice), to the row's outputs.  weights(entries, index of the first, w): 0 for
@@ -394,6 +459,7 @@ constexpr int kAllLanes = 256, kAllWaves = kAllLanes / 64;
 // is small as it is.
 constexpr int kAllRegions = 8, kShortRow = 8192;
 constexpr int kFinishLanes = 256;
+constexpr int kMaxSplits = 64;
 
 // The largest of the lanes' entries.
 template <class S>
@@ -464,10 +530,10 @@ __device__ void sum_regions(const Row<S>& row, int regions, int k0, int n, const
     while (k < n) close();
 }
 
-// The row's draw from its regions' parts; scaled: room for their weights relative to the row's largest score.
+// The row's draw from its regions' parts, at most kLanes.
 template <int kLanes, class S>
 __device__ void finish_row(const SampleArgs& a, int64_t r, const Row<S>& row, const Parameters& par, const Part* parts,
-                           int regions, double* scaled, PickShared<kLanes>& sh) {
+                           int regions, PickShared<kLanes>& sh) {
     using X = typename S::X;
     uint32_t top_key = 0;
     u64 count = 0;
@@ -494,26 +560,16 @@ __device__ void finish_row(const SampleArgs& a, int64_t r, const Row<S>& row, co
     }
     Exponent ex;
     ex.set(top, par.scale());
-    for (int k = threadIdx.x; k < regions; k += kLanes)
-        scaled[k] = parts[k].count ? parts[k].weight * ex.weight(S::value(parts[k].key)) : 0.0;
-    __syncthreads();
-    double sum = 0.0;
-    int target = 0;
-    for (int k = 0; k < regions; ++k) {
-        sum += scaled[k];
-        if (scaled[k] > 0.0) target = k;
+    double mine = 0.0;
+    if ((int)threadIdx.x < regions) {
+        const Part p = parts[threadIdx.x];
+        mine = p.count ? p.weight * ex.weight(S::value(p.key)) : 0.0;
     }
-    const double t = ((double)(a.rnd[r] >> 11) * 0x1p-53) * sum;
-    double before = 0.0;
-    for (int k = 0; k < target; ++k) {
-        if (before + scaled[k] > t) {
-            target = k;
-            break;
-        }
-        before += scaled[k];
-    }
+    const double u = (double)(a.rnd[r] >> 11) * 0x1p-53;
+    double sum, before;
+    const int target = target_region<kLanes>(mine, u, false, &sum, &before, sh);
     pick_in_region<kLanes>(
-        row, Region(row.groups, regions, target), t - before, Draw{a, r, (double)top, (double)par.T, sum, count},
+        row, Region(row.groups, regions, target), u * sum - before, Draw{a, r, (double)top, (double)par.T, sum, count},
         [&](const X (&v)[S::V], int, double (&w)[S::V]) { ex.weights(v, w); }, sh);
 }
 
@@ -523,7 +579,6 @@ __global__ void __launch_bounds__(kAllLanes) all_kernel(SampleArgs a, int splits
     using S = Scores<kType>;
     constexpr int kRegions = kAllWaves * kAllRegions;
     __shared__ Part own[kRegions];
-    __shared__ double scaled[kRegions];
     __shared__ PickShared<kAllLanes> sh;
     const int64_t r = a.row0 + blockIdx.x / splits;
     const int s = blockIdx.x % splits, wave = wave_index();
@@ -536,22 +591,19 @@ __global__ void __launch_bounds__(kAllLanes) all_kernel(SampleArgs a, int splits
     const int each = a.N <= kShortRow ? 1 : kAllRegions;
     sum_regions(row, kAllWaves * each, wave * each, each, par, own + wave * each);
     __syncthreads();
-    finish_row<kAllLanes>(a, r, row, par, own, kAllWaves * each, scaled, sh);
+    finish_row<kAllLanes>(a, r, row, par, own, kAllWaves * each, sh);
 }
-
-constexpr int kMaxSplits = 64;
 
 template <int kType>
 __global__ void __launch_bounds__(kFinishLanes) finish_kernel(SampleArgs a, int splits, const Part* parts) {
     using S = Scores<kType>;
     __shared__ Part own[kMaxSplits * kAllWaves];
-    __shared__ double scaled[kMaxSplits * kAllWaves];
     __shared__ PickShared<kFinishLanes> sh;
     const int64_t r = a.row0 + blockIdx.x;
     const int regions = splits * kAllWaves;
     for (int k = threadIdx.x; k < regions; k += kFinishLanes) own[k] = parts[r * regions + k];
     __syncthreads();
-    finish_row<kFinishLanes>(a, r, Row<S>(a, r), Parameters(a, r), own, regions, scaled, sh);
+    finish_row<kFinishLanes>(a, r, Row<S>(a, r), Parameters(a, r), own, regions, sh);
 }
 
 // ------------------------------------------------------------------ filters
@@ -559,7 +611,15 @@ __global__ void __launch_bounds__(kFinishLanes) finish_kernel(SampleArgs a, int 
 constexpr int kCutLanes = 1024;
 constexpr int kBins = 2048;
 constexpr int kList = 2048;
-constexpr int kRank = 64;
+constexpr int kRank = 256;
+
+// x as a whole number, rounded towards zero: NaN to 0, what is too large to the largest, as the instruction has it and
+// the language does not say.
+__device__ __forceinline__ uint32_t saturate(float x) {
+    uint32_t r;
+    asm("v_cvt_u32_f32 %0, %1" : "=v"(r) : "v"(x));
+    return r;
+}
 
 // An entry's place in the order (descending score, ascending index): smaller is earlier.
 __device__ __forceinline__ u64 place_of(uint32_t key, uint32_t index) { return ((u64)~key << 32) | index; }
@@ -571,10 +631,10 @@ template <class F>
 __device__ __forceinline__ uint32_t least_key(uint32_t lo, uint32_t hi, F reached) {
     const int lane = threadIdx.x & 63;
     while (hi - lo > 1) {
-        const uint32_t step = (hi - lo) / 65 + 1;
+        const uint32_t step = ((hi - lo - 1) >> 6) + 1;  // 64 steps reach hi
         const u64 probe = (u64)lo + (u64)step * (lane + 1);
         const u64 m = __ballot(probe >= hi || reached((uint32_t)probe));
-        const int first = m ? __ffsll(m) - 1 : 64;
+        const int first = __ffsll(m) - 1;
         const u64 up = (u64)lo + (u64)step * (first + 1);
         lo += step * first;
         hi = up < hi ? (uint32_t)up : hi;
@@ -582,13 +642,13 @@ __device__ __forceinline__ uint32_t least_key(uint32_t lo, uint32_t hi, F reache
     return hi;
 }
 
-template <int kLanes>
+template <int kLanes, bool kLists = true>
 struct CutShared {
     static constexpr int kWaves = kLanes / 64;
     uint32_t count[kBins];
     u64 weight[kBins];
-    u64 list[kList], list_w[kList];
-    u64 some[kRank], some_w[kRank];
+    u64 list[kLists ? kList : 1], list_w[kLists ? kList : 1];
+    ulonglong2 some[kRank];  // place, weight
     u64 wave_c[kWaves], wave_w[kWaves];
     u64 above_c, above_w, in_bin, found, found_w, lo64, hi64;
     uint32_t bin, listed, lo, hi;
@@ -596,21 +656,72 @@ struct CutShared {
     PickShared<kLanes> pick;
 };
 
+// A row's extent: its largest and smallest score's keys and the number of its entries.
+struct Extent {
+    uint32_t top, low, count, unused;
+};
+
+// What a row's filters ask for.
+template <class S>
+struct Goal {
+    using X = typename S::X;
+    bool nothing;     // no entries, or parameters out of range
+    bool one;         // the first of the largest scores is all that is kept
+    bool by_k, by_p;  // top-k leaves something out, top-p does
+    u64 k;
+    double p, q;
+    X top;
+    uint32_t top_key;
+    Exponent ex;
+    float bins_per;  // distance bins per unit of score
+    int unit;        // whole-number weights are w 2^unit, rounded: the sums stay below 2^62
+    __device__ __forceinline__ Goal(const Parameters& par, const Extent& e, int n) {
+        nothing = e.count == 0 || par.bad;
+        one = par.T == 0.0f || par.q > 1.0f || par.p <= 0.0f || par.k == 1;
+        by_k = !nothing && !one && par.k > 0 && (uint32_t)par.k < e.count;
+        by_p = !nothing && !one && par.p < 1.0f;
+        k = (u64)par.k;
+        p = (double)par.p;
+        q = (double)par.q;
+        top_key = e.top;
+        top = S::value(e.top);
+        ex.set(top, par.T == 0.0f ? 1.0 : par.scale());
+        // weights past 24 T below the top add less than 4e-11 each: their bins need no width of their own; a count
+        // alone goes by the scores' range
+        const float reach = 24.0f * par.T, spread = S::below(top, S::value(e.low));
+        bins_per = (float)(kBins - 1) / (par.p < 1.0f && reach < spread ? reach : spread);
+        const int bits = n > 1 ? 32 - __clz(n - 1) : 0;
+        unit = bits < 11 ? 51 : 62 - bits;
+    }
+    // The last place whose weight is at least min-p; every lane of a wavefront calls it.
+    __device__ __forceinline__ u64 last_by_weight() const {
+        if (one) return place_of(top_key, 0xFFFFFFFFu);
+        if (!(q > 0.0)) return ~(u64)0;
+        const uint32_t k_ = least_key(S::key(S::kMasked), top_key,
+                                      [&](uint32_t c) { return ex.weight(S::value(c)) >= q; });
+        return place_of(k_, 0xFFFFFFFFu);
+    }
+};
+
 // Where a row's filters end: the place of the last kept entry.
-template <int kLanes, class S>
+template <int kLanes, class S, bool kLists = true>
 struct Cutter {
     using X = typename S::X;
     static constexpr int kWaves = kLanes / 64, kOwn = kBins / kLanes;  // bins of a lane
     const Row<S>& row;
     Region mine;  // this wavefront's
-    Exponent ex;
+    const Exponent& ex;
     X top;
     uint32_t top_key;
-    float bins_per;  // distance bins per unit of score
-    int unit;        // whole-number weights are w 2^unit, rounded: the sums stay below 2^62
-    bool weights;    // top-p is on
-    bool filled;     // the bins hold the row's distances
-    CutShared<kLanes>& sh;
+    float bins_per;
+    int unit;
+    bool weights;  // top-p is on
+    bool filled;   // the bins hold the row's distances
+    CutShared<kLanes, kLists>& sh;
+    __device__ __forceinline__ Cutter(const Row<S>& r, const Region& g, const Goal<S>& goal,
+                                      CutShared<kLanes, kLists>& shared)
+        : row(r), mine(g), ex(goal.ex), top(goal.top), top_key(goal.top_key), bins_per(goal.bins_per), unit(goal.unit),
+          weights(goal.by_p), filled(false), sh(shared) {}
 
     // w 2^unit, rounded, is what adding 2^(52 - unit) leaves in the low bits (unit <= 51, w <= 1).
     __device__ __forceinline__ u64 fixed(double w) const {
@@ -621,8 +732,16 @@ struct Cutter {
     // Distance bins: equal scores share one, and a lower score is never in an earlier one.  NaN (inf - inf, or the
     // top itself where bins_per is infinite) goes to the first bin, what is past the range to the last.
     __device__ __forceinline__ uint32_t bin_of(X v) const {
-        const float b = S::below(top, v) * bins_per;
-        return b >= (float)(kBins - 1) ? kBins - 1 : b > 0.0f ? (uint32_t)b : 0u;
+        const uint32_t b = saturate(S::below(top, v) * bins_per);
+        return b < kBins - 1 ? b : kBins - 1;
+    }
+    // A bin's keys: from the smallest that is in it or an earlier one to the last before the earlier ones'.
+    __device__ __forceinline__ uint32_t first_key(uint32_t bin) const {
+        return least_key(S::key(S::kMasked), top_key, [&](uint32_t k) { return bin_of(S::value(k)) <= bin; });
+    }
+    __device__ __forceinline__ uint32_t last_key(uint32_t bin) const {
+        if (bin == 0) return top_key;
+        return least_key(S::key(S::kMasked), top_key, [&](uint32_t k) { return bin_of(S::value(k)) < bin; }) - 1;
     }
     template <class B>
     __device__ __forceinline__ void walk(B body) const {
@@ -672,10 +791,8 @@ struct Cutter {
                 }
             });
         }
-        for (int o = 32; o > 0; o >>= 1) {
-            far += (uint32_t)__shfl_xor((int)far, o, 64);
-            far_w += __shfl_xor(far_w, o, 64);
-        }
+        far = wave_sum(far);
+        far_w = wave_sum(far_w);
         if (lane == 0) {
             atomicAdd(&sh.count[kBins - 1], far);
             atomicAdd(&sh.weight[kBins - 1], far_w);
@@ -688,7 +805,7 @@ struct Cutter {
         u64 w = 0;
 #pragma unroll
         for (int i = 0; i < kOwn; ++i) w += sh.weight[threadIdx.x + i * kLanes];
-        for (int o = 32; o > 0; o >>= 1) w += __shfl_xor(w, o, 64);
+        w = wave_sum(w);
         if ((threadIdx.x & 63) == 0) sh.wave_w[wave_index()] = w;
         __syncthreads();
         w = 0;
@@ -762,7 +879,7 @@ struct Cutter {
                     for (int e = 0; e < S::V; ++e)
                         if (x[e] == v && ++at == number) sh.found = place_of(S::key(v), (uint32_t)(first + e));
                 }
-                seen += (uint32_t)__shfl((int)scan, 63, 64);
+                seen += last_lane(scan);
             });
         }
         __syncthreads();
@@ -771,8 +888,25 @@ struct Cutter {
         return r;
     }
 
-    // The cut among the listed entries: split by the bits of their places until at most kRank are left, which a
-    // wavefront ranks.
+    // How many of `number` entries of the same score v the cut takes.
+    __device__ u64 equal_needed(X v, u64 number, bool by_weight, u64 want, double goal, u64 above_c, u64 above_w,
+                                u64* up_to) const {
+        const u64 w = fixed_of(v);
+        u64 r;
+        if (by_weight) {
+            const double q = (goal - (double)above_w) / (double)w;  // w > 0: the weight reaches goal here
+            r = q < 1.0 ? 1 : q >= (double)number ? number : (u64)q;
+            while (r > 1 && (double)(above_w + (r - 1) * w) >= goal) --r;
+            while (r < number && (double)(above_w + r * w) < goal) ++r;
+        } else {
+            r = want - above_c;
+        }
+        *up_to = above_w + r * w;
+        return r;
+    }
+
+    // The cut among the listed entries: split by the bits of their places until at most kRank are left, which
+    // are ranked.
     __device__ u64 cut_list(uint32_t number, bool by_weight, u64 want, double goal, u64 above_c, u64 above_w, u64* up_to) {
         const int tid = threadIdx.x;
         u64 lo = 0, hi = ~(u64)0;  // places still in question
@@ -817,25 +951,25 @@ struct Cutter {
             const u64 end = lo + (((u64)1 << shift) - 1);
             hi = end < hi ? end : hi;
         }
-        // at most kRank entries: one wavefront's lanes, each against all
+        // at most kRank entries: each against all
         if (tid == 0) sh.listed = 0;
         __syncthreads();
         for (uint32_t i = tid; i < number; i += kLanes) {
             const u64 p = sh.list[i];
             if (p < lo || p > hi) continue;
             const uint32_t at = atomicAdd(&sh.listed, 1u);
-            sh.some[at] = p;
-            sh.some_w[at] = sh.list_w[i];
+            sh.some[at] = ulonglong2{p, sh.list_w[i]};
         }
         __syncthreads();
         const uint32_t left = sh.listed;
         if ((uint32_t)tid < left) {
-            const u64 p = sh.some[tid], w = sh.some_w[tid];
+            const u64 p = sh.some[tid].x, w = sh.some[tid].y;
             u64 before = above_c, before_w = above_w;
             for (uint32_t j = 0; j < left; ++j) {
-                const bool earlier = sh.some[j] < p;
+                const ulonglong2 other = sh.some[j];
+                const bool earlier = other.x < p;
                 before += earlier;
-                before_w += earlier ? sh.some_w[j] : 0;
+                before_w += earlier ? other.y : 0;
             }
             if (by_weight ? (double)before_w < goal && (double)(before_w + w) >= goal : before + 1 == want) {
                 sh.found = p;
@@ -854,11 +988,7 @@ struct Cutter {
     __device__ u64 cut(bool by_weight, u64 want, double goal, u64* up_to) {
         const int tid = threadIdx.x;
         cross(by_weight, want, goal, 0, 0);
-        // the bin's keys: from the smallest that is in it or an earlier one to the last before the earlier ones
-        const uint32_t bin = sh.bin, none = S::key(S::kMasked);
-        uint32_t lo = least_key(none, top_key, [&](uint32_t k) { return bin_of(S::value(k)) <= bin; });
-        uint32_t hi = bin == 0 ? top_key
-                               : least_key(none, top_key, [&](uint32_t k) { return bin_of(S::value(k)) < bin; }) - 1;
+        uint32_t lo = first_key(sh.bin), hi = last_key(sh.bin);
         for (;;) {
             const u64 above_c = sh.above_c, above_w = sh.above_w;
             __syncthreads();
@@ -873,6 +1003,10 @@ struct Cutter {
             X least = to, most = from;
             uint32_t any = 0;
             walk([&](const X (&v)[S::V], int first) {
+                bool reach = false;
+#pragma unroll
+                for (int e = 0; e < S::V; ++e) reach = reach || v[e] >= from;
+                if (!__any(reach)) return;
 #pragma unroll
                 for (int e = 0; e < S::V; ++e) {
                     if (v[e] >= from && v[e] <= to) {
@@ -898,18 +1032,7 @@ struct Cutter {
             }
             if (lo == hi) {  // equal scores: as many of them as it takes, in index order
                 const X v = S::value(lo);
-                const u64 w = fixed_of(v);
-                u64 r;
-                if (by_weight) {
-                    const double q = (goal - (double)above_w) / (double)w;  // w > 0: the weight reaches goal here
-                    r = q < 1.0 ? 1 : q >= (double)number ? number : (u64)q;
-                    while (r > 1 && (double)(above_w + (r - 1) * w) >= goal) --r;
-                    while (r < number && (double)(above_w + r * w) < goal) ++r;
-                } else {
-                    r = want - above_c;
-                }
-                *up_to = above_w + r * w;
-                return nth_equal(v, r);
+                return nth_equal(v, equal_needed(v, number, by_weight, want, goal, above_c, above_w, up_to));
             }
             // split the range of keys: 2,048 bins from the largest key down
             const int shift = 32 - __clz((hi - lo) >> 11);
@@ -933,30 +1056,21 @@ struct Cutter {
     }
 
     // The last kept place by all filters.
-    __device__ u64 last_kept(const Parameters& par, uint32_t eligible) {
-        if (par.T == 0.0f || par.q > 1.0f || par.p <= 0.0f) return nth_equal(top, 1);  // one entry is kept always
-        const bool by_k = par.k > 0 && (uint32_t)par.k < eligible, by_p = par.p < 1.0f;
-        u64 last = ~(u64)0;
-        weights = by_p;
-        u64 total = 0;
+    __device__ u64 last_kept(const Goal<S>& goal) {
+        u64 last = ~(u64)0, total = 0;
 #pragma unroll 1
-        for (int by_weight = by_k ? 0 : 1; by_weight <= (by_p ? 1 : 0); ++by_weight) {
+        for (int by_weight = goal.by_k ? 0 : 1; by_weight <= (goal.by_p ? 1 : 0); ++by_weight) {
             // top-k's cut first: top-p goes by the weight of the first k, and reaches its share of that before the last
             // of them
-            if (!filled) fill_bins(by_k && !by_weight);
-            if (by_weight && !by_k) total = total_weight();
+            if (!filled) fill_bins(goal.by_k && !by_weight);
+            if (by_weight && !goal.by_k) total = total_weight();
             u64 up_to = 0;
-            const u64 at = cut(by_weight != 0, (u64)par.k, (double)par.p * (double)total, &up_to);
+            const u64 at = cut(by_weight != 0, goal.k, goal.p * (double)total, &up_to);
             last = at < last ? at : last;
             total = up_to;
         }
-        if (par.q > 0.0f) {
-            const uint32_t k = least_key(S::key(S::kMasked), top_key,
-                                         [&](uint32_t p) { return ex.weight(S::value(p)) >= (double)par.q; });
-            const u64 at = place_of(k, 0xFFFFFFFFu);
-            last = at < last ? at : last;
-        }
-        return last;
+        const u64 at = goal.last_by_weight();
+        return at < last ? at : last;
     }
 };
 
@@ -974,7 +1088,7 @@ struct Kept {
         return v > edge || (v == edge && i <= edge_at && v != S::kMasked);
     }
     // Weights of a lane's entries, 0 for those not kept; skipped where no lane of the wavefront keeps one.
-    __device__ __forceinline__ bool weights(const Exponent& ex, bool greedy, const X (&v)[S::V], int first,
+    __device__ __forceinline__ bool weights(const Exponent& ex, bool one, const X (&v)[S::V], int first,
                                             double (&w)[S::V], uint32_t* count) const {
         bool keep[S::V], some = false;
 #pragma unroll
@@ -985,111 +1099,384 @@ struct Kept {
 #pragma unroll
         for (int e = 0; e < S::V; ++e) w[e] = 0.0;
         if (!__any(some)) return false;
-        if (!greedy) ex.weights(v, w);
+        if (!one) ex.weights(v, w);
 #pragma unroll
         for (int e = 0; e < S::V; ++e) {
-            w[e] = !keep[e] ? 0.0 : greedy ? 1.0 : w[e];
+            w[e] = !keep[e] ? 0.0 : one ? 1.0 : w[e];
             *count += __popcll(__ballot(keep[e]));
         }
         return true;
     }
 };
 
-template <int kType>
-__global__ void __launch_bounds__(kCutLanes) cut_kernel(SampleArgs a) {
-    using S = Scores<kType>;
+// The extent of a wavefront's groups.
+template <class S>
+__device__ Extent extent_of(const Row<S>& row, const Region& g) {
     using X = typename S::X;
-    constexpr int kWaves = kCutLanes / 64;
-    __shared__ CutShared<kCutLanes> sh;
-    const int tid = threadIdx.x, wave = wave_index(), lane = tid & 63;
-    const int64_t r = a.row0 + blockIdx.x;
-    const Row<S> row(a, r);
-    const Parameters par(a, r);
-    const Region mine(row.groups, kWaves, wave);
-
-    // the largest score, the smallest one, the number of entries
-    X most = S::kMasked, least = S::value(0xFFFFFFFFu - (kType == HX_SCORE_I32 ? 0u : 0x7FFFFFu));
-    uint32_t eligible = 0;
-    row.walk(mine.lo, mine.hi, [&](const X (&v)[S::V], int) {
+    X most = S::kMasked, least = S::value(0xFFFFFFFFu - (std::is_same<X, float>::value ? 0x7FFFFFu : 0u));
+    uint32_t count = 0;
+    row.walk(g.lo, g.hi, [&](const X (&v)[S::V], int) {
 #pragma unroll
         for (int e = 0; e < S::V; ++e) {
             most = S::larger(most, v[e]);
             least = v[e] != S::kMasked && v[e] < least ? v[e] : least;
-            eligible += __popcll(__ballot(v[e] != S::kMasked));
+            count += __popcll(__ballot(v[e] != S::kMasked));
         }
     });
+    return Extent{wave_max(S::key(most)), ~wave_max(~S::key(least)), count, 0u};
+}
+
+// Weight and number of a wavefront's kept entries.
+template <class S>
+__device__ Part sum_kept(const Row<S>& row, const Region& g, const Kept<S>& kept, const Goal<S>& goal) {
+    double sum = 0.0;
+    uint32_t number = 0;
+    row.walk(g.lo, g.hi, [&](const typename S::X (&v)[S::V], int first) {
+        double w[S::V];
+        if (!kept.weights(goal.ex, goal.one, v, first, w, &number)) return;
+#pragma unroll
+        for (int e = 0; e < S::V; ++e) sum += w[e];
+    });
+    return Part{wave_sum(sum), 0u, number};
+}
+
+// The row's draw among its kept entries, from its regions' parts, at most kLanes.
+template <int kLanes, class S>
+__device__ void draw_kept(const SampleArgs& a, int64_t r, const Row<S>& row, const Parameters& par, const Kept<S>& kept,
+                          const Goal<S>& goal, const Part* parts, int regions, PickShared<kLanes>& sh) {
+    u64 count = 0;
+    if (!goal.one) {
+        // each wavefront for itself
+        for (int k = threadIdx.x & 63; k < regions; k += 64) count += parts[k].count;
+        count = wave_sum(count);
+    }
+    const double u = (double)(a.rnd[r] >> 11) * 0x1p-53;
+    double sum, before;
+    const int target = target_region<kLanes>((int)threadIdx.x < regions ? parts[threadIdx.x].weight : 0.0, u, goal.one,
+                                             &sum, &before, sh);
+    const double t = goal.one ? 0.0 : u * sum;  // one: the first of equal weights
+    const Draw draw{a, r, (double)goal.top, (double)par.T, goal.one ? 1.0 : sum, goal.one ? 1 : count};
+    pick_in_region<kLanes>(
+        row, Region(row.groups, regions, target), t - before, draw,
+        [&](const typename S::X (&v)[S::V], int first, double (&w)[S::V]) {
+            uint32_t n = 0;
+            kept.weights(goal.ex, goal.one, v, first, w, &n);
+        },
+        sh);
+}
+
+// A row by one workgroup.
+template <class S>
+__device__ void cut_row(const SampleArgs& a, int64_t r, const Row<S>& row, const Parameters& par,
+                        CutShared<kCutLanes>& sh) {
+    constexpr int kWaves = kCutLanes / 64;
+    const int tid = threadIdx.x, wave = wave_index(), lane = tid & 63;
+    const Region mine(row.groups, kWaves, wave);
+    const Extent own = extent_of(row, mine);
     if (tid == 0) {
         sh.listed = sh.hi = 0;
         sh.lo = 0xFFFFFFFFu;
     }
     __syncthreads();
-    if (eligible) {
-        const uint32_t up = wave_max(S::key(most)), down = ~wave_max(~S::key(least));
-        if (lane == 0) {
-            atomicAdd(&sh.listed, eligible);
-            atomicMax(&sh.hi, up);
-            atomicMin(&sh.lo, down);
-        }
+    if (own.count && lane == 0) {
+        atomicAdd(&sh.listed, own.count);
+        atomicMax(&sh.hi, own.top);
+        atomicMin(&sh.lo, own.low);
     }
     __syncthreads();
-    eligible = sh.listed;
-    if (eligible == 0 || par.bad) {
+    const Goal<S> goal(par, Extent{sh.hi, sh.lo, sh.listed, 0u}, row.n);
+    if (goal.nothing) {
         if (tid == 0) write_nothing(a, r);
         return;
     }
-    const uint32_t top_key = sh.hi;
-    const X top = S::value(top_key), low = S::value(sh.lo);
     __syncthreads();
-
-    const bool greedy = par.T == 0.0f;
-    // weights past 24 T below the top add less than 4e-11 each: their bins need no width of their own; a count alone
-    // goes by the scores' range
-    const float reach = 24.0f * par.T, spread = S::below(top, low);
-    Exponent ex;
-    ex.set(top, greedy ? 0.0 : par.scale());
-    Cutter<kCutLanes, S> cut{row, mine, ex, top, top_key,
-                             (float)(kBins - 1) / (par.p < 1.0f && reach < spread ? reach : spread), 0, false,
-                             false, sh};
-    const int bits = row.n > 1 ? 32 - __clz(row.n - 1) : 0;
-    cut.unit = bits < 11 ? 51 : 62 - bits;
-    const Kept<S> kept(cut.last_kept(par, eligible));
-
-    // weight and number of the kept entries, by region
-    double sum = 0.0;
-    uint32_t number = 0;
-    row.walk(mine.lo, mine.hi, [&](const X (&v)[S::V], int first) {
-        double w[S::V];
-        if (!kept.weights(ex, greedy, v, first, w, &number)) return;
-#pragma unroll
-        for (int e = 0; e < S::V; ++e) sum += w[e];
-    });
-    sum = wave_sum(sum);
-    if (lane == 0) sh.part[wave] = Part{sum, 0u, number};
+    Cutter<kCutLanes, S> cut(row, mine, goal, sh);
+    const Kept<S> kept(cut.last_kept(goal));
+    const Part p = sum_kept(row, mine, kept, goal);
+    if (lane == 0) sh.part[wave] = p;
     __syncthreads();
-    double all = 0.0;
-    u64 count = 0;
-    int target = 0;
-    for (int k = 0; k < kWaves; ++k) {
-        all += sh.part[k].weight;
-        count += sh.part[k].count;
-        if (sh.part[k].weight > 0.0) target = k;
+    draw_kept<kCutLanes>(a, r, row, par, kept, goal, sh.part, kWaves, sh.pick);
+}
+
+template <int kType>
+__global__ void __launch_bounds__(kCutLanes) cut_kernel(SampleArgs a) {
+    using S = Scores<kType>;
+    __shared__ CutShared<kCutLanes> sh;
+    const int64_t r = a.row0 + blockIdx.x;
+    cut_row(a, r, Row<S>(a, r), Parameters(a, r), sh);
+}
+
+// ------------------------------------------------------------------ filters, a row split over workgroups
+//
+// The same steps, each a launch of its own over all splits of all rows; what the splits find meets in the
+// row's SplitRow, and each workgroup works out for itself what follows from that:
+//   extent_kernel  the splits' extents; clears the row's bins and lists
+//   fill_kernel    counts and weights of the distance bins, summed in the row's
+//   gather_kernel  the entries of the bins in which the cuts fall, into the row's lists
+//   sum_kernel     the cuts, from the lists; weight and number of the regions' kept entries
+//   draw_kernel    a workgroup per row: the draw
+// A bin with more entries than a list holds is of one score as a rule (16-bit scores): the cut is then a number of
+// them, and the split in which the last one is finds it.  A row with a longer list of different scores is cut as a
+// whole by draw_kernel.
+
+constexpr int kSplitLanes = 512, kSplitWaves = kSplitLanes / 64;
+
+struct SplitRow {
+    uint32_t count[kBins];
+    u64 weight[kBins];
+    u64 list[2][kList];  // places: of top-k's bin, of top-p's
+    u64 above_c, above_w[2];  // before those bins: entries (top-k), weight
+    u64 last;                 // place of the last kept entry
+    uint32_t listed[2], lo[2], hi[2];  // entries of those bins, their range of keys
+    uint32_t found[2][kMaxSplits];     // entries of each split
+    Extent extent[kMaxSplits];
+    Part part[kMaxSplits * kSplitWaves];
+    __device__ __forceinline__ bool fits(int c) const { return listed[c] <= kList; }
+    __device__ __forceinline__ bool cut_here() const {
+        return (fits(0) || lo[0] == hi[0]) && (fits(1) || lo[1] == hi[1]);
     }
-    const double t = ((double)(a.rnd[r] >> 11) * 0x1p-53) * all;
-    double before = 0.0;
-    for (int k = 0; k < target; ++k) {
-        if (before + sh.part[k].weight > t) {
-            target = k;
-            break;
+};
+
+template <class S>
+__device__ __forceinline__ Extent row_extent(const SplitRow& w, int splits) {
+    const int lane = threadIdx.x & 63;  // kMaxSplits lanes
+    Extent e{0u, 0xFFFFFFFFu, 0u, 0u};
+    if (lane < splits) e = w.extent[lane];
+    if (e.count == 0) e = Extent{0u, 0xFFFFFFFFu, 0u, 0u};
+    return Extent{wave_max(e.top), ~wave_max(~e.low), wave_sum(e.count), 0u};
+}
+
+template <int kType>
+__global__ void __launch_bounds__(kSplitLanes) extent_kernel(SampleArgs a, int splits, SplitRow* rows) {
+    using S = Scores<kType>;
+    __shared__ Extent own[kSplitWaves];
+    const int64_t i = blockIdx.x / splits, r = a.row0 + i;
+    const int s = blockIdx.x % splits, wave = wave_index();
+    SplitRow& w = rows[i];
+    for (int b = s * kSplitLanes + threadIdx.x; b < kBins; b += splits * kSplitLanes) {
+        w.count[b] = 0;
+        w.weight[b] = 0;
+    }
+    if (s == 0 && threadIdx.x < 2) {
+        w.listed[threadIdx.x] = w.hi[threadIdx.x] = 0;
+        w.lo[threadIdx.x] = 0xFFFFFFFFu;
+    }
+    const Row<S> row(a, r);
+    const Extent e = extent_of(row, Region(row.groups, splits * kSplitWaves, s * kSplitWaves + wave));
+    if ((threadIdx.x & 63) == 0) own[wave] = e.count ? e : Extent{0u, 0xFFFFFFFFu, 0u, 0u};
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        Extent all = own[0];
+        for (int k = 1; k < kSplitWaves; ++k) {
+            all.top = own[k].top > all.top ? own[k].top : all.top;
+            all.low = own[k].low < all.low ? own[k].low : all.low;
+            all.count += own[k].count;
         }
-        before += sh.part[k].weight;
+        w.extent[s] = all;
     }
-    pick_in_region<kCutLanes>(
-        row, Region(row.groups, kWaves, target), t - before, Draw{a, r, (double)top, (double)par.T, all, count},
-        [&](const X (&v)[S::V], int first, double (&w)[S::V]) {
-            uint32_t n = 0;
-            kept.weights(ex, greedy, v, first, w, &n);
-        },
-        sh.pick);
+}
+
+template <int kType>
+__global__ void __launch_bounds__(kSplitLanes) fill_kernel(SampleArgs a, int splits, SplitRow* rows) {
+    using S = Scores<kType>;
+    __shared__ CutShared<kSplitLanes, false> sh;
+    const int64_t i = blockIdx.x / splits, r = a.row0 + i;
+    const int s = blockIdx.x % splits;
+    SplitRow& w = rows[i];
+    const Row<S> row(a, r);
+    const Goal<S> goal(Parameters(a, r), row_extent<S>(w, splits), row.n);
+    if (!goal.by_k && !goal.by_p) return;
+    Cutter<kSplitLanes, S, false> cut(row, Region(row.groups, splits * kSplitWaves, s * kSplitWaves + wave_index()), goal, sh);
+    cut.fill_bins(goal.by_k);
+    for (int b = threadIdx.x; b < kBins; b += kSplitLanes) {
+        const uint32_t c = sh.count[b];
+        const u64 v = sh.weight[b];
+        if (c) atomicAdd(&w.count[b], c);
+        if (v) atomicAdd(&w.weight[b], v);
+    }
+}
+
+template <int kType>
+__global__ void __launch_bounds__(kSplitLanes) gather_kernel(SampleArgs a, int splits, SplitRow* rows) {
+    using S = Scores<kType>;
+    using X = typename S::X;
+    __shared__ CutShared<kSplitLanes> sh;
+    __shared__ uint32_t listed[2], base[2];
+    const int64_t i = blockIdx.x / splits, r = a.row0 + i;
+    const int s = blockIdx.x % splits, tid = threadIdx.x;
+    SplitRow& w = rows[i];
+    const Row<S> row(a, r);
+    const Goal<S> goal(Parameters(a, r), row_extent<S>(w, splits), row.n);
+    if (!goal.by_k && !goal.by_p) return;
+    Cutter<kSplitLanes, S> cut(row, Region(row.groups, splits * kSplitWaves, s * kSplitWaves + wave_index()), goal, sh);
+    for (int b = tid; b < kBins; b += kSplitLanes) {
+        sh.count[b] = w.count[b];
+        sh.weight[b] = w.weight[b];
+    }
+    if (tid < 2) listed[tid] = 0;
+    __syncthreads();
+    // keys [lo, hi] of the bins of either cut; none: an empty range
+    uint32_t lo[2] = {0xFFFFFFFFu, 0xFFFFFFFFu}, hi[2] = {0u, 0u};
+    u64 least = 0, most = 0;  // bounds of the first k's weight
+    if (goal.by_k) {
+        cut.cross(false, goal.k, 0.0, 0, 0);
+        const uint32_t bin = sh.bin;
+        lo[0] = cut.first_key(bin);
+        hi[0] = cut.last_key(bin);
+        least = sh.above_w;
+        most = least + sh.weight[bin];
+        if (s == 0 && tid == 0) {
+            w.above_c = sh.above_c;
+            w.above_w[0] = least;
+        }
+        __syncthreads();
+    }
+    if (goal.by_p) {
+        if (!goal.by_k) least = most = cut.total_weight();
+        // top-p's cut is between the goals that these bounds give (at least half a unit: a weight reaches it)
+        const double g = goal.p * (double)least;
+        cut.cross(true, 0, g < 0.5 ? 0.5 : g, 0, 0);
+        hi[1] = cut.last_key(sh.bin);
+        if (s == 0 && tid == 0) w.above_w[1] = sh.above_w;
+        __syncthreads();
+        if (goal.by_k) {
+            const double up = goal.p * (double)most;
+            cut.cross(true, 0, up < 0.5 ? 0.5 : up, 0, 0);
+        }
+        lo[1] = cut.first_key(sh.bin);
+        __syncthreads();
+    }
+    // sh.list and sh.list_w hold the two lists until they are copied
+    const X from[2] = {S::value(lo[0]), S::value(lo[1])}, to[2] = {S::value_up(hi[0]), S::value_up(hi[1])};
+    const bool on[2] = {goal.by_k, goal.by_p};
+    X low[2] = {to[0], to[1]}, high[2] = {from[0], from[1]};
+    bool any[2] = {false, false};
+    cut.walk([&](const X (&v)[S::V], int first) {
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {
+            if (!on[c]) continue;
+            u64* list = c ? sh.list_w : sh.list;
+            bool reach = false;
+#pragma unroll
+            for (int e = 0; e < S::V; ++e) reach = reach || v[e] >= from[c];
+            if (!__any(reach)) continue;
+#pragma unroll
+            for (int e = 0; e < S::V; ++e) {
+                if (v[e] >= from[c] && v[e] <= to[c]) {
+                    low[c] = v[e] < low[c] ? v[e] : low[c];
+                    high[c] = v[e] > high[c] ? v[e] : high[c];
+                    any[c] = true;
+                    const uint32_t at = atomicAdd(&listed[c], 1u);
+                    if (at < kList) list[at] = place_of(S::key(v[e]), (uint32_t)(first + e));
+                }
+            }
+        }
+    });
+#pragma unroll
+    for (int c = 0; c < 2; ++c) {
+        if (!__any(any[c])) continue;
+        const uint32_t k0 = ~wave_max(any[c] ? ~S::key(low[c]) : 0u), k1 = wave_max(any[c] ? S::key(high[c]) : 0u);
+        if ((tid & 63) == 0) {
+            atomicMin(&w.lo[c], k0);
+            atomicMax(&w.hi[c], k1);
+        }
+    }
+    __syncthreads();
+    if (tid < 2) {
+        w.found[tid][s] = listed[tid];
+        base[tid] = listed[tid] ? atomicAdd(&w.listed[tid], listed[tid]) : 0u;
+    }
+    __syncthreads();
+    for (int c = 0; c < 2; ++c) {
+        const uint32_t n = listed[c] < kList ? listed[c] : kList, at = base[c];
+        const u64* list = c ? sh.list_w : sh.list;
+        for (uint32_t k = tid; k < n && at + k < kList; k += kSplitLanes) w.list[c][at + k] = list[k];
+    }
+}
+
+template <int kType>
+__global__ void __launch_bounds__(kSplitLanes) sum_kernel(SampleArgs a, int splits, SplitRow* rows) {
+    using S = Scores<kType>;
+    using X = typename S::X;
+    __shared__ CutShared<kSplitLanes> sh;
+    const int64_t i = blockIdx.x / splits, r = a.row0 + i;
+    const int s = blockIdx.x % splits, tid = threadIdx.x, region = s * kSplitWaves + wave_index();
+    SplitRow& w = rows[i];
+    const Row<S> row(a, r);
+    const Goal<S> goal(Parameters(a, r), row_extent<S>(w, splits), row.n);
+    if (goal.nothing || !w.cut_here()) return;
+    const Region mine(row.groups, splits * kSplitWaves, region);
+    Cutter<kSplitLanes, S> cut(row, mine, goal, sh);
+    const u64 q = goal.last_by_weight();
+    u64 last = q, total = 0;
+    int writer = 0;  // the split that knows the row's last place: all do, but of equal scores
+#pragma unroll 1
+    for (int c = goal.by_k ? 0 : 1; c <= (goal.by_p ? 1 : 0); ++c) {
+        if (c && !goal.by_k) {
+            for (int b = tid; b < kBins; b += kSplitLanes) sh.weight[b] = w.weight[b];
+            __syncthreads();
+            total = cut.total_weight();
+        }
+        const uint32_t number = w.listed[c];
+        const double share = goal.p * (double)total;
+        const u64 above_c = c ? 0 : w.above_c, above_w = w.above_w[c];
+        u64 up_to = 0, at;
+        if (number <= kList) {
+            for (uint32_t k = tid; k < number; k += kSplitLanes) {
+                const u64 p = w.list[c][k];
+                sh.list[k] = p;
+                sh.list_w[k] = cut.fixed_of(S::value(key_at(p)));
+            }
+            at = cut.cut_list(number, c != 0, goal.k, share, above_c, above_w, &up_to);
+            writer = 0;
+        } else {
+            // the earlier splits keep all of these, the later ones none
+            const uint32_t key = w.lo[c];
+            const X v = S::value(key);
+            const u64 need = cut.equal_needed(v, number, c != 0, goal.k, share, above_c, above_w, &up_to);
+            const int lane = tid & 63;  // kMaxSplits lanes
+            const uint32_t here = lane < splits ? w.found[c][lane] : 0;
+            const u64 to = wave_scan((u64)here);
+            const int split = __ffsll(__ballot(to >= need)) - 1;
+            at = place_of(key, s < split ? 0xFFFFFFFFu : 0u);
+            if (s == split) at = cut.nth_equal(v, need - (u64)__shfl(to - here, split, 64));
+            writer = q < place_of(key, 0u) ? 0 : split;
+        }
+        last = at < last ? at : last;
+        total = up_to;
+    }
+    if (s == writer && tid == 0) w.last = last;
+    const Part p = sum_kept(row, mine, Kept<S>(last), goal);
+    if ((tid & 63) == 0) w.part[region] = p;
+}
+
+template <int kType>
+__global__ void __launch_bounds__(kCutLanes) draw_kernel(SampleArgs a, int splits, const SplitRow* rows) {
+    using S = Scores<kType>;
+    __shared__ CutShared<kCutLanes> sh;
+    const int64_t r = a.row0 + blockIdx.x;
+    const SplitRow& w = rows[blockIdx.x];
+    const Row<S> row(a, r);
+    const Parameters par(a, r);
+    const Goal<S> goal(par, row_extent<S>(w, splits), row.n);
+    if (goal.nothing) {
+        if (threadIdx.x == 0) write_nothing(a, r);
+        return;
+    }
+    if (!w.cut_here()) {
+        cut_row(a, r, row, par, sh);
+        return;
+    }
+    // the draw takes kSplitLanes lanes: one for every region
+    if (threadIdx.x >= kSplitLanes) return;
+    static_assert(kMaxSplits * kSplitWaves <= kSplitLanes, "a lane for every region");
+    Part* parts = reinterpret_cast<Part*>(sh.list);
+    static_assert(sizeof(sh.list) >= sizeof(w.part), "the parts fit the list's room");
+    const int regions = splits * kSplitWaves;
+    if ((int)threadIdx.x < regions) parts[threadIdx.x] = w.part[threadIdx.x];
+    __syncthreads();
+    draw_kept<kSplitLanes>(a, r, row, par, Kept<S>(w.last), goal, parts, regions,
+                           reinterpret_cast<PickShared<kSplitLanes>&>(sh.weight));
 }
 
 // Workgroups a row without filters is split into: until the chip has two for every CU, with 4,096 entries
@@ -1101,22 +1488,52 @@ int splits_of(int32_t R, int32_t N) {
     return s < 1 ? 1 : (int)s;
 }
 
+// Workgroups a row with filters is split into, 4,096 entries or more to each; 0: one of kCutLanes lanes and a single
+// launch.  Splitting takes five launches, in which every split works out the row's cuts for itself, and pays while the
+// rows alone leave most of the chip idle: 16 rows of 131,072 entries 52 against 132 us, 64 of 65,536 as fast either way,
+// 256 of 32,768 93 against 49.
+int cut_splits_of(int32_t R, int32_t N) {
+    if (N < 16384 || (int64_t)R * 1000 > N) return 0;
+    int64_t s = 1024 / R, most = N / 4096;
+    if (s > most) s = most;
+    if (s > kMaxSplits) s = kMaxSplits;
+    return s < 1 ? 1 : (int)s;
+}
+
 constexpr int32_t kRowsPerLaunch = 1 << 20;  // a grid has fewer than 2^32 lanes
+constexpr int32_t kSplitRows = 256;          // rows of SplitRow that the workspace has
+
+size_t cut_workspace(int32_t R, int32_t N) {
+    return cut_splits_of(R, N) ? sizeof(SplitRow) * (R < kSplitRows ? R : kSplitRows) : 0;
+}
 
 template <int kType>
 hipError_t launch(SampleArgs a, void* workspace, hipStream_t s) {
-    const int splits = splits_of(a.R, a.N);  // 1 where a second launch is needed
-    Part* parts = static_cast<Part*>(workspace);
-    for (int64_t r0 = 0; r0 < a.R; r0 += kRowsPerLaunch) {
-        const unsigned rows = (unsigned)(a.R - r0 < kRowsPerLaunch ? a.R - r0 : kRowsPerLaunch);
+    const bool filters = a.top_k || a.top_p || a.min_p;
+    const int splits = filters ? cut_splits_of(a.R, a.N) : splits_of(a.R, a.N);
+    // several launches share the workspace: one after the other on the stream
+    const int32_t per = filters && splits ? kSplitRows : kRowsPerLaunch;
+    for (int64_t r0 = 0; r0 < a.R; r0 += per) {
+        const unsigned rows = (unsigned)(a.R - r0 < per ? a.R - r0 : per);
         a.row0 = r0;
-        if (a.top_k || a.top_p || a.min_p) {
+        if (!filters) {
+            Part* parts = static_cast<Part*>(workspace);  // more splits than one: few rows
+            hipLaunchKernelGGL(all_kernel<kType>, dim3(rows * splits), dim3(kAllLanes), 0, s, a, splits, parts);
+            if (splits > 1)
+                hipLaunchKernelGGL(finish_kernel<kType>, dim3(rows), dim3(kFinishLanes), 0, s, a, splits, parts);
+        } else if (!splits) {
             hipLaunchKernelGGL(cut_kernel<kType>, dim3(rows), dim3(kCutLanes), 0, s, a);
-            continue;
+        } else {
+            SplitRow* w = static_cast<SplitRow*>(workspace);
+            const dim3 grid(rows * splits), block(kSplitLanes);
+            hipLaunchKernelGGL(extent_kernel<kType>, grid, block, 0, s, a, splits, w);
+            if (a.top_k || a.top_p) {
+                hipLaunchKernelGGL(fill_kernel<kType>, grid, block, 0, s, a, splits, w);
+                hipLaunchKernelGGL(gather_kernel<kType>, grid, block, 0, s, a, splits, w);
+            }
+            hipLaunchKernelGGL(sum_kernel<kType>, grid, block, 0, s, a, splits, w);
+            hipLaunchKernelGGL(draw_kernel<kType>, dim3(rows), dim3(kCutLanes), 0, s, a, splits, w);
         }
-        hipLaunchKernelGGL(all_kernel<kType>, dim3(rows * splits), dim3(kAllLanes), 0, s, a, splits, parts);
-        if (splits > 1)
-            hipLaunchKernelGGL(finish_kernel<kType>, dim3(rows), dim3(kFinishLanes), 0, s, a, splits, parts);
     }
     return hipGetLastError();
 }
@@ -1125,8 +1542,8 @@ hipError_t launch(SampleArgs a, void* workspace, hipStream_t s) {
 
 size_t sample_workspace_bytes(int32_t R, int32_t N) {
     const int splits = splits_of(R, N);
-    const size_t parts = splits > 1 ? (size_t)R * splits * kAllWaves * sizeof(Part) : 0;
-    return (parts + 511) & ~(size_t)255;
+    const size_t parts = splits > 1 ? (size_t)R * splits * kAllWaves * sizeof(Part) : 0, cuts = cut_workspace(R, N);
+    return ((parts > cuts ? parts : cuts) + 511) & ~(size_t)255;
 }
 
 hipError_t launch_sample(const SampleArgs& a, void* workspace, hipStream_t s) {
