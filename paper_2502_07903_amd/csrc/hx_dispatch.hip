@@ -91,6 +91,42 @@ __device__ u64 block_scan(u64 v, u64* wave_sum) {
     return v;
 }
 
+// Sums over the chunks (of `number`, rows of kKeys words) of this lane's key, tid mod kKeys: those before chunk `at`
+// and all.  Four lanes share a key's chunks, with eight loads in flight each; part: LDS.
+template <class W>
+__device__ void chunk_sums(const W* words, int keys, int number, int at, u64 (*part)[2][kKeys], u64* before, u64* all) {
+    const int key = threadIdx.x % kKeys, share = threadIdx.x / kKeys;
+    constexpr int kShares = kLanes / kKeys, kFlight = 8;
+    u64 b = 0, a = 0;
+    if (key < keys) {
+        for (int t0 = share; t0 < number; t0 += kShares * kFlight) {
+            W v[kFlight];
+#pragma unroll
+            for (int k = 0; k < kFlight; ++k) {
+                const int t = t0 + k * kShares;
+                v[k] = t < number ? words[(int64_t)t * kKeys + key] : 0;
+            }
+#pragma unroll
+            for (int k = 0; k < kFlight; ++k) {
+                a += v[k];
+                b += t0 + k * kShares < at ? v[k] : 0;
+            }
+        }
+    }
+    part[share][0][key] = b;
+    part[share][1][key] = a;
+    __syncthreads();
+    b = a = 0;
+#pragma unroll
+    for (int k = 0; k < kShares; ++k) {
+        b += part[k][0][key];
+        a += part[k][1][key];
+    }
+    __syncthreads();
+    *before = b;
+    *all = a;
+}
+
 // Rows are worked on by chunks of whole 1,024s, a workgroup each, and at most kChunks of them, so that a chunk
 // can add up what the others counted by itself.
 constexpr int kChunks = 128;
@@ -128,10 +164,16 @@ __device__ u64 flow_ends(const RouteArgs& a, u64* ends, u64* wave_sum, int* edge
     const int per = (edges + kLanes - 1) / kLanes;
     const int lo = tid * per < edges ? tid * per : edges, hi = lo + per < edges ? lo + per : edges;
     u64 mine = 0;
-    for (int e = lo; e < hi; ++e) {
-        const int32_t f = a.kv_flow[(int64_t)e * a.nets + a.cand];
-        mine += f > 0 ? (u64)f : 0;
-        ends[e] = mine;
+    constexpr int kAhead = kEdgesLds / kLanes;  // loads in flight
+    for (int e0 = lo; e0 < hi; e0 += kAhead) {
+        int32_t f[kAhead];
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k) f[k] = e0 + k < hi ? a.kv_flow[(int64_t)(e0 + k) * a.nets + a.cand] : 0;
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k) {
+            mine += f[k] > 0 ? (u64)f[k] : 0;
+            if (e0 + k < hi) ends[e0 + k] = mine;
+        }
     }
     const u64 scan = block_scan(mine, wave_sum);
     for (int e = lo; e < hi; ++e) ends[e] += scan - mine;
@@ -254,15 +296,10 @@ __global__ void __launch_bounds__(kLanes) route_lists_kernel(RouteArgs a) {
     const int32_t* node = side ? a.o.decode : a.o.prefill;
     int32_t* order = side ? a.o.d_order : a.o.p_order;
     if (!order) return;
-    u64 before = 0, all = 0;
-    if (tid < nodes) {
-        const uint32_t* c = a.counts + (int64_t)side * gridDim.x * kKeys + tid;
-        for (int t = 0; t < (int)gridDim.x; ++t) {
-            const uint32_t v = c[(int64_t)t * kKeys];
-            before += t < (int)blockIdx.x ? v : 0;
-            all += v;
-        }
-    }
+    u64 before, all;
+    chunk_sums(a.counts + (int64_t)side * gridDim.x * kKeys, nodes, (int)gridDim.x, (int)blockIdx.x,
+               reinterpret_cast<u64(*)[2][kKeys]>(s.wave), &before, &all);
+    if (tid >= nodes) before = all = 0;
     if (tid <= nodes) s.run[tid] = all;
     __syncthreads();
     run_starts(s, wave_sum, nodes, blockIdx.x == 0 ? (side ? a.o.d_base : a.o.p_base) : nullptr);
@@ -299,6 +336,7 @@ struct KvArgs {
     int64_t max_slots;
     uint8_t* placed;
     const uint8_t* done;
+    uint32_t factor, shift;  // x / block_size = (x factor >> 32) >> shift for x < 2^31, block_size > 1
     KvRow* row;    // [n_rows]
     u64* total;    // [chunks][kKeys] blocks of each replica's rows
     u64* tokens;   // [chunks]
@@ -376,12 +414,19 @@ __global__ void __launch_bounds__(kLanes) kv_totals_kernel(KvArgs a) {
     if (tid < a.p.n_replicas) a.total[(int64_t)blockIdx.x * kKeys + tid] = sum[tid];
 }
 
+// x / block_size for x < 2^31.  With 2^(l-1) < b <= 2^l and factor = ceil(2^(31+l) / b), factor b is above 2^(31+l) by
+// less than b <= 2^l, so that x factor / 2^(31+l) is above x / b by less than 1 / b, and has the same whole part.
+__device__ __forceinline__ uint32_t over_block(const KvArgs& a, uint32_t x) {
+    return a.p.block_size == 1 ? x : __umulhi(x, a.factor) >> a.shift;
+}
+
 // Slot of token t (counted over all rows) of row i, which starts at token first: its block is the table's, or new
 // and entered into it by its first token.
 __device__ __forceinline__ int64_t slot_of(const KvArgs& a, int64_t i, const KvRow& row, int64_t t, int64_t first) {
     if (!row.number) return -1;
     const uint32_t b = (uint32_t)a.p.block_size, pos = (uint32_t)(row.held + (int32_t)(t - first));
-    const uint32_t col = pos / b, off = pos - col * b, b0 = ((uint32_t)row.held + b - 1) / b;
+    const uint32_t col = over_block(a, pos), off = pos - col * b;
+    const uint32_t b0 = row.held ? over_block(a, (uint32_t)row.held - 1) + 1 : 0;
     int32_t* entry = a.r.block_table + i * a.r.table_stride + col;
     int32_t block;
     if (col < b0) {
@@ -405,10 +450,11 @@ __global__ void __launch_bounds__(kLanes) kv_rows_kernel(KvArgs a, int fill) {
     __shared__ int32_t start[kOne ? kLanes : 1];  // kOne: the rows' first tokens and data, for the fill
     __shared__ KvRow own[kOne ? kLanes : 1];
     const int tid = threadIdx.x, R = a.p.n_replicas;
+    u64 before = 0, total;
+    if (!kOne)
+        chunk_sums(a.total, R, (int)blockIdx.x, (int)blockIdx.x, reinterpret_cast<u64(*)[2][kKeys]>(s.wave), &before,
+                   &total);
     if (tid < R) {
-        u64 before = 0;
-        if (!kOne)
-            for (int t = 0; t < (int)blockIdx.x; ++t) before += a.total[(int64_t)t * kKeys + tid];
         const Replica q = kOne ? Replica(a.p, tid) : Replica(a.free0[tid], a.room[tid]);
         s.run[tid] = before;
         moved[tid] = 0;
@@ -417,8 +463,8 @@ __global__ void __launch_bounds__(kLanes) kv_rows_kernel(KvArgs a, int fill) {
     }
     if (tid == 0) carry = 0;
     if (!kOne && kPlace) {
-        const u64 before = block_scan(tid < (int)blockIdx.x ? a.tokens[tid] : 0, wave_sum);  // at most kChunks <= kLanes
-        if (tid == kLanes - 1) carry = before;
+        const u64 tokens = block_scan(tid < (int)blockIdx.x ? a.tokens[tid] : 0, wave_sum);  // at most kChunks <= kLanes
+        if (tid == kLanes - 1) carry = tokens;
     }
     __syncthreads();
     const int64_t i0 = (int64_t)blockIdx.x * a.chunk;
@@ -490,35 +536,54 @@ __device__ __forceinline__ void write_free(const KvArgs& a, bool place) {
             a.p.free_out[q] = (int32_t)(place ? a.free0[q] - (int64_t)a.moved[q] : a.free0[q] + (int64_t)a.moved[q]);
 }
 
-// Slots of kFillTokens tokens.
-constexpr int kFillLanes = 256, kFillTokens = 2048;
+// Slots of kFillTokens tokens: row by row where few rows have them, otherwise each token looks for its row.  Most of a
+// workgroup's time is the chain of its loads (the search, the rows, the blocks), so the chain is kept short.
+constexpr int kFillLanes = 256, kFillTokens = 2048, kFillRows = 8;
 __global__ void __launch_bounds__(kFillLanes) place_fill_kernel(KvArgs a) {
+    __shared__ int64_t start[kFillRows + 1];
+    __shared__ KvRow rows[kFillRows];
     write_free(a, true);
-    const int64_t n = a.tok_base[a.r.n_rows] < a.max_slots ? a.tok_base[a.r.n_rows] : a.max_slots;
+    const int64_t all = a.tok_base[a.r.n_rows];
     const int64_t t0 = (int64_t)blockIdx.x * kFillTokens;
+    // the last rows whose tokens start at or before the first token (lanes 0 to 31 of a wavefront) and the last one (32
+    // to 63), by 32 probes a round: row lo does, row hi (or none) does not
+    const int lane = threadIdx.x & 63, half = lane >> 5;
+    const int64_t want = half ? t0 + kFillTokens - 1 : t0;
+    int64_t lo = 0, hi = a.r.n_rows;
+    while (__any(hi - lo > 1)) {
+        const int64_t step = hi - lo > 1 ? ((hi - lo - 1) >> 5) + 1 : 1, probe = lo + step * ((lane & 31) + 1);
+        const u64 past = __ballot(probe >= hi || a.tok_base[probe] > want);
+        const int first = __ffs((unsigned)(past >> (32 * half))) - 1;
+        const int64_t up = lo + step * (first + 1);
+        lo += step * first;
+        hi = up < hi ? up : hi;
+    }
+    const int64_t first = __shfl(lo, 0, 64), last = __shfl(lo, 32, 64);
+    const int64_t n = all < a.max_slots ? all : a.max_slots;
     if (t0 >= n) return;
     const int64_t t1 = t0 + kFillTokens < n ? t0 + kFillTokens : n;
-    // the last rows that start at or before the first and the last token
-    int64_t ends[2];
-#pragma unroll
-    for (int k = 0; k < 2; ++k) {
-        const int64_t t = k ? t1 - 1 : t0;
-        int64_t lo = 0, hi = a.r.n_rows - 1;
-        while (lo < hi) {
-            const int64_t mid = (lo + hi + 1) / 2;
-            if (a.tok_base[mid] <= t) lo = mid;
-            else hi = mid - 1;
+    if (last - first < kFillRows) {
+        const int number = (int)(last - first) + 1;
+        if ((int)threadIdx.x <= number) start[threadIdx.x] = a.tok_base[first + threadIdx.x];
+        if ((int)threadIdx.x < number) rows[threadIdx.x] = a.row[first + threadIdx.x];
+        __syncthreads();
+        for (int k = 0; k < number; ++k) {
+            const KvRow row = rows[k];
+            const int64_t from = start[k] > t0 ? start[k] : t0, to = start[k + 1] < t1 ? start[k + 1] : t1;
+#pragma unroll 8
+            for (int64_t t = from + threadIdx.x; t < to; t += kFillLanes)
+                a.slots[t] = slot_of(a, first + k, row, t, start[k]);
         }
-        ends[k] = lo;
+        return;
     }
     for (int64_t t = t0 + threadIdx.x; t < t1; t += kFillLanes) {
-        int64_t lo = ends[0], hi = ends[1];
-        while (lo < hi) {
-            const int64_t mid = (lo + hi + 1) / 2;
-            if (a.tok_base[mid] <= t) lo = mid;
-            else hi = mid - 1;
+        int64_t at = first, end = last;
+        while (at < end) {
+            const int64_t mid = (at + end + 1) / 2;
+            if (a.tok_base[mid] <= t) at = mid;
+            else end = mid - 1;
         }
-        a.slots[t] = slot_of(a, lo, a.row[lo], t, a.tok_base[lo]);
+        a.slots[t] = slot_of(a, at, a.row[at], t, a.tok_base[at]);
     }
 }
 
@@ -562,6 +627,11 @@ KvArgs kv_args(const hx_kv_pool& p, const hx_kv_rows& r, void* workspace) {
     a.r = r;
     a.chunk = c.rows;
     a.chunks = c.number;
+    uint32_t l = 1;
+    while ((1u << l) < (uint32_t)p.block_size) ++l;
+    const uint64_t one = (uint64_t)1 << (31 + l);
+    a.factor = p.block_size == 1 ? 0 : (uint32_t)((one + (uint32_t)p.block_size - 1) / (uint32_t)p.block_size);
+    a.shift = l - 1;
     a.row = reinterpret_cast<KvRow*>(b + w.row);
     a.total = reinterpret_cast<u64*>(b + w.total);
     a.tokens = reinterpret_cast<u64*>(b + w.tokens);
