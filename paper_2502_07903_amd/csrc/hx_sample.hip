@@ -13,7 +13,7 @@
 // With filters (cut_kernel, a workgroup per row): all three keep a prefix of the order (descending score,
 // ascending index), so the kept set is everything up to one entry's place in it.  That entry is found by
 // counting, for top-k, and by adding whole-number weights, for top-p (64-bit sums: no order of addition
-// changes them), in 2,048 bins of the distance from m.  The entries of the bin in which the cut falls, if
+// changes them), in 1,024 bins of the distance from m.  The entries of the bin in which the cut falls, if
 // at most kList, go to a list in LDS, which is split by the bits of their places until a wavefront can rank
 // the rest; a longer bin is split again by the keys' bits over the row.  min-p's bound is a search over the
 // keys.
@@ -51,7 +51,8 @@ struct Scores<HX_SCORE_I32> {
     static __device__ __forceinline__ X value_up(uint32_t k) { return value(k); }
     static __device__ __forceinline__ float below(X m, X x) { return (float)((uint32_t)m - (uint32_t)x); }
 };
-// Floats: NaN is masked (clean makes it -inf; unpack leaves it); keys are sign and magnitude in two's-complement order, -0 as +0.
+// Floats: NaN is masked (clean makes it -inf; unpack leaves it); keys are sign and magnitude in two's-complement
+// order, -0 as +0.
 struct FloatScores {
     using X = float;
     static constexpr X kMasked = -INFINITY, kLeast = -FLT_MAX;
@@ -61,7 +62,9 @@ struct FloatScores {
         const uint32_t b = __float_as_uint(x + 0.0f);
         return b ^ ((uint32_t)((int32_t)b >> 31) | 0x80000000u);
     }
-    static __device__ __forceinline__ X value(uint32_t k) { return __uint_as_float(k & 0x80000000u ? k ^ 0x80000000u : ~k); }
+    static __device__ __forceinline__ X value(uint32_t k) {
+        return __uint_as_float(k & 0x80000000u ? k ^ 0x80000000u : ~k);
+    }
     // The largest score whose key is at most k: the key of -0, which no score has, would compare equal to +0.
     static __device__ __forceinline__ X value_up(uint32_t k) { return value(k == 0x7FFFFFFFu ? k - 1 : k); }
     static __device__ __forceinline__ float below(X m, X x) { return m - x; }
@@ -225,17 +228,28 @@ struct Row {
         }
     }
     // body(entries, index of the first) for a wavefront's groups [lo, hi), 64 at a time and all lanes together (masked
-    // entries where a lane has no group), the next 64 groups being fetched meanwhile.  Without kClean, NaN stays.
-    template <bool kClean = true, class B>
+    // entries where a lane has no group).  The next kAhead times 64 groups are fetched meanwhile: one where the body is
+    // long, four where the loads' latency would be the time.  Without kClean, NaN stays.
+    template <int kAhead, bool kClean = true, class B>
     __device__ __forceinline__ void walk(int lo, int hi, B body) const {
         const int lane = threadIdx.x & 63;
-        uint4 next = fetch(lo + lane);
-        for (int g = lo + lane; g - lane < hi; g += 64) {
-            const uint4 q = next;
-            next = fetch(g + 64);
-            X v[V];
-            entries<kClean>(g, hi, q, v);
-            body(v, first(g));
+        uint4 next[kAhead];
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k) next[k] = fetch(lo + 64 * k + lane);
+        for (int g = lo + lane; g - lane < hi; g += 64 * kAhead) {
+            uint4 q[kAhead];
+#pragma unroll
+            for (int k = 0; k < kAhead; ++k) {
+                q[k] = next[k];
+                next[k] = fetch(g + 64 * (kAhead + k));
+            }
+#pragma unroll
+            for (int k = 0; k < kAhead; ++k) {
+                if (k > 0 && g - lane + 64 * k >= hi) continue;
+                X v[V];
+                entries<kClean>(g + 64 * k, hi, q[k], v);
+                body(v, first(g + 64 * k));
+            }
         }
     }
 };
@@ -495,7 +509,7 @@ __device__ void sum_regions(const Row<S>& row, int regions, int k0, int n, const
         ++k;
         end += per;
     };
-    row.template walk<false>(first.lo, last.hi, [&](const X (&v)[S::V], int) {
+    row.template walk<1, false>(first.lo, last.hi, [&](const X (&v)[S::V], int) {
         if (g0 >= end) close();
         g0 += 64;
 #pragma unroll
@@ -608,8 +622,10 @@ __global__ void __launch_bounds__(kFinishLanes) finish_kernel(SampleArgs a, int 
 
 // ------------------------------------------------------------------ filters
 
-constexpr int kCutLanes = 1024;
-constexpr int kBins = 2048;
+// Lanes of a row: 512 with at most 128 registers, so that two rows share a CU and one computes while the other waits
+// (1,024 rows of 32,768 bf16 with top-p and min-p: 139 us; 1,024 lanes, one row a CU: 207; 256 lanes: 154).
+constexpr int kCutLanes = 512, kCutWaves = kCutLanes / 64;
+constexpr int kBinBits = 10, kBins = 1 << kBinBits;
 constexpr int kList = 2048;
 constexpr int kRank = 256;
 
@@ -735,17 +751,28 @@ struct Cutter {
         const uint32_t b = saturate(S::below(top, v) * bins_per);
         return b < kBins - 1 ? b : kBins - 1;
     }
-    // A bin's keys: from the smallest that is in it or an earlier one to the last before the earlier ones'.
-    __device__ __forceinline__ uint32_t first_key(uint32_t bin) const {
-        return least_key(S::key(S::kMasked), top_key, [&](uint32_t k) { return bin_of(S::value(k)) <= bin; });
+    // The keys of bins b0 to b1: from the smallest whose bin is at most b1 to the last before those whose bin is below
+    // b0.  Both ends at once, by 32 probes a round each; every lane of a wavefront calls it.
+    __device__ __forceinline__ void keys_of(uint32_t b0, uint32_t b1, uint32_t* first, uint32_t* last) const {
+        const int lane = threadIdx.x & 63, half = lane >> 5;
+        const uint32_t want = half ? b0 : b1 + 1;  // bins below this one (none is below bin 0)
+        uint32_t lo = S::key(S::kMasked), hi = half && b0 == 0 ? top_key + 1 : top_key;
+        if (half && b0 == 0) lo = top_key;
+        while (__any(hi - lo > 1)) {
+            const uint32_t step = hi - lo > 1 ? ((hi - lo - 1) >> 5) + 1 : 1;
+            const u64 probe = (u64)lo + (u64)step * ((lane & 31) + 1);
+            const u64 m = __ballot(probe >= hi || bin_of(S::value((uint32_t)probe)) < want);
+            const int at = __ffs((unsigned)(m >> (32 * half))) - 1;
+            const u64 up = (u64)lo + (u64)step * (at + 1);
+            lo += step * at;
+            hi = up < hi ? (uint32_t)up : hi;
+        }
+        *first = (uint32_t)__builtin_amdgcn_readlane((int)hi, 0);
+        *last = (uint32_t)__builtin_amdgcn_readlane((int)hi, 32) - 1;
     }
-    __device__ __forceinline__ uint32_t last_key(uint32_t bin) const {
-        if (bin == 0) return top_key;
-        return least_key(S::key(S::kMasked), top_key, [&](uint32_t k) { return bin_of(S::value(k)) < bin; }) - 1;
-    }
-    template <class B>
+    template <int kAhead, class B>
     __device__ __forceinline__ void walk(B body) const {
-        row.walk(mine.lo, mine.hi, body);
+        row.template walk<kAhead>(mine.lo, mine.hi, body);
     }
 
     __device__ __forceinline__ void clear_bins() {
@@ -766,7 +793,7 @@ struct Cutter {
         uint32_t far = 0;
         u64 far_w = 0;
         if (weights) {
-            walk([&](const X (&v)[S::V], int) {
+            walk<1>([&](const X (&v)[S::V], int) {
                 double w[S::V];
                 ex.weights(v, w);
 #pragma unroll
@@ -782,7 +809,7 @@ struct Cutter {
                 }
             });
         } else {
-            walk([&](const X (&v)[S::V], int) {
+            walk<2>([&](const X (&v)[S::V], int) {
 #pragma unroll
                 for (int e = 0; e < S::V; ++e) {
                     const uint32_t b = bin_of(v[e]);
@@ -833,9 +860,11 @@ struct Cutter {
         }
         __syncthreads();
         u64 ec = above_c + sc - sum_c, ew = above_w + sw - sum_w;
-        for (int k = 0; k < wave; ++k) {
-            ec += sh.wave_c[k];
-            ew += sh.wave_w[k];
+#pragma unroll
+        for (int k = 0; k < kWaves; ++k) {
+            const u64 c_ = sh.wave_c[k], w_ = sh.wave_w[k];
+            ec += k < wave ? c_ : 0;
+            ew += k < wave ? w_ : 0;
         }
 #pragma unroll
         for (int i = 0; i < kOwn; ++i) {
@@ -857,17 +886,21 @@ struct Cutter {
     __device__ u64 nth_equal(X v, u64 number) {
         const int wave = wave_index(), lane = threadIdx.x & 63;
         u64 n = 0;
-        walk([&](const X (&x)[S::V], int) {
+        walk<2>([&](const X (&x)[S::V], int) {
 #pragma unroll
             for (int e = 0; e < S::V; ++e) n += __popcll(__ballot(x[e] == v));
         });
         if (lane == 0) sh.wave_c[wave] = n;
         __syncthreads();
         u64 before = 0;
-        for (int k = 0; k < wave; ++k) before += sh.wave_c[k];
+#pragma unroll
+        for (int k = 0; k < kWaves; ++k) {
+            const u64 c = sh.wave_c[k];
+            before += k < wave ? c : 0;
+        }
         if (before < number && before + n >= number) {
             u64 seen = before;
-            walk([&](const X (&x)[S::V], int first) {
+            walk<1>([&](const X (&x)[S::V], int first) {
                 if (seen >= number) return;
                 uint32_t here = 0;
 #pragma unroll
@@ -907,7 +940,8 @@ struct Cutter {
 
     // The cut among the listed entries: split by the bits of their places until at most kRank are left, which
     // are ranked.
-    __device__ u64 cut_list(uint32_t number, bool by_weight, u64 want, double goal, u64 above_c, u64 above_w, u64* up_to) {
+    __device__ u64 cut_list(uint32_t number, bool by_weight, u64 want, double goal, u64 above_c, u64 above_w,
+                            u64* up_to) {
         const int tid = threadIdx.x;
         u64 lo = 0, hi = ~(u64)0;  // places still in question
         if (tid == 0) sh.in_bin = number;
@@ -934,7 +968,7 @@ struct Cutter {
             __syncthreads();
             lo = sh.lo64;
             hi = sh.hi64;
-            const u64 spread = (hi - lo) >> 11;
+            const u64 spread = (hi - lo) >> kBinBits;
             const int shift = spread ? 64 - __clzll(spread) : 0;
             for (uint32_t i = tid; i < number; i += kLanes) {
                 const u64 p = sh.list[i];
@@ -965,6 +999,7 @@ struct Cutter {
         if ((uint32_t)tid < left) {
             const u64 p = sh.some[tid].x, w = sh.some[tid].y;
             u64 before = above_c, before_w = above_w;
+#pragma unroll 4
             for (uint32_t j = 0; j < left; ++j) {
                 const ulonglong2 other = sh.some[j];
                 const bool earlier = other.x < p;
@@ -988,7 +1023,8 @@ struct Cutter {
     __device__ u64 cut(bool by_weight, u64 want, double goal, u64* up_to) {
         const int tid = threadIdx.x;
         cross(by_weight, want, goal, 0, 0);
-        uint32_t lo = first_key(sh.bin), hi = last_key(sh.bin);
+        uint32_t lo, hi;
+        keys_of(sh.bin, sh.bin, &lo, &hi);
         for (;;) {
             const u64 above_c = sh.above_c, above_w = sh.above_w;
             __syncthreads();
@@ -1002,7 +1038,7 @@ struct Cutter {
             const X from = S::value(lo), to = S::value_up(hi);
             X least = to, most = from;
             uint32_t any = 0;
-            walk([&](const X (&v)[S::V], int first) {
+            walk<2>([&](const X (&v)[S::V], int first) {
                 bool reach = false;
 #pragma unroll
                 for (int e = 0; e < S::V; ++e) reach = reach || v[e] >= from;
@@ -1034,10 +1070,10 @@ struct Cutter {
                 const X v = S::value(lo);
                 return nth_equal(v, equal_needed(v, number, by_weight, want, goal, above_c, above_w, up_to));
             }
-            // split the range of keys: 2,048 bins from the largest key down
-            const int shift = 32 - __clz((hi - lo) >> 11);
+            // split the range of keys: bins from the largest key down
+            const int shift = 32 - __clz((hi - lo) >> kBinBits);
             clear_bins();
-            walk([&](const X (&v)[S::V], int) {
+            walk<1>([&](const X (&v)[S::V], int) {
 #pragma unroll
                 for (int e = 0; e < S::V; ++e) {
                     const uint32_t k = S::key(v[e]);
@@ -1115,7 +1151,7 @@ __device__ Extent extent_of(const Row<S>& row, const Region& g) {
     using X = typename S::X;
     X most = S::kMasked, least = S::value(0xFFFFFFFFu - (std::is_same<X, float>::value ? 0x7FFFFFu : 0u));
     uint32_t count = 0;
-    row.walk(g.lo, g.hi, [&](const X (&v)[S::V], int) {
+    row.template walk<4>(g.lo, g.hi, [&](const X (&v)[S::V], int) {
 #pragma unroll
         for (int e = 0; e < S::V; ++e) {
             most = S::larger(most, v[e]);
@@ -1131,7 +1167,7 @@ template <class S>
 __device__ Part sum_kept(const Row<S>& row, const Region& g, const Kept<S>& kept, const Goal<S>& goal) {
     double sum = 0.0;
     uint32_t number = 0;
-    row.walk(g.lo, g.hi, [&](const typename S::X (&v)[S::V], int first) {
+    row.template walk<2>(g.lo, g.hi, [&](const typename S::X (&v)[S::V], int first) {
         double w[S::V];
         if (!kept.weights(goal.ex, goal.one, v, first, w, &number)) return;
 #pragma unroll
@@ -1169,9 +1205,8 @@ __device__ void draw_kept(const SampleArgs& a, int64_t r, const Row<S>& row, con
 template <class S>
 __device__ void cut_row(const SampleArgs& a, int64_t r, const Row<S>& row, const Parameters& par,
                         CutShared<kCutLanes>& sh) {
-    constexpr int kWaves = kCutLanes / 64;
     const int tid = threadIdx.x, wave = wave_index(), lane = tid & 63;
-    const Region mine(row.groups, kWaves, wave);
+    const Region mine(row.groups, kCutWaves, wave);
     const Extent own = extent_of(row, mine);
     if (tid == 0) {
         sh.listed = sh.hi = 0;
@@ -1195,11 +1230,11 @@ __device__ void cut_row(const SampleArgs& a, int64_t r, const Row<S>& row, const
     const Part p = sum_kept(row, mine, kept, goal);
     if (lane == 0) sh.part[wave] = p;
     __syncthreads();
-    draw_kept<kCutLanes>(a, r, row, par, kept, goal, sh.part, kWaves, sh.pick);
+    draw_kept<kCutLanes>(a, r, row, par, kept, goal, sh.part, kCutWaves, sh.pick);
 }
 
 template <int kType>
-__global__ void __launch_bounds__(kCutLanes) cut_kernel(SampleArgs a) {
+__global__ void __launch_bounds__(kCutLanes, 4) cut_kernel(SampleArgs a) {  // four wavefronts a SIMD: 128 registers
     using S = Scores<kType>;
     __shared__ CutShared<kCutLanes> sh;
     const int64_t r = a.row0 + blockIdx.x;
@@ -1286,7 +1321,8 @@ __global__ void __launch_bounds__(kSplitLanes) fill_kernel(SampleArgs a, int spl
     const Row<S> row(a, r);
     const Goal<S> goal(Parameters(a, r), row_extent<S>(w, splits), row.n);
     if (!goal.by_k && !goal.by_p) return;
-    Cutter<kSplitLanes, S, false> cut(row, Region(row.groups, splits * kSplitWaves, s * kSplitWaves + wave_index()), goal, sh);
+    const Region mine(row.groups, splits * kSplitWaves, s * kSplitWaves + wave_index());
+    Cutter<kSplitLanes, S, false> cut(row, mine, goal, sh);
     cut.fill_bins(goal.by_k);
     for (int b = threadIdx.x; b < kBins; b += kSplitLanes) {
         const uint32_t c = sh.count[b];
@@ -1301,7 +1337,7 @@ __global__ void __launch_bounds__(kSplitLanes) gather_kernel(SampleArgs a, int s
     using S = Scores<kType>;
     using X = typename S::X;
     __shared__ CutShared<kSplitLanes> sh;
-    __shared__ uint32_t listed[2], base[2];
+    __shared__ uint32_t listed[2], base[2], ends[4];  // ends: least keys, largest keys
     const int64_t i = blockIdx.x / splits, r = a.row0 + i;
     const int s = blockIdx.x % splits, tid = threadIdx.x;
     SplitRow& w = rows[i];
@@ -1313,7 +1349,10 @@ __global__ void __launch_bounds__(kSplitLanes) gather_kernel(SampleArgs a, int s
         sh.count[b] = w.count[b];
         sh.weight[b] = w.weight[b];
     }
-    if (tid < 2) listed[tid] = 0;
+    if (tid < 2) {
+        listed[tid] = ends[2 + tid] = 0;
+        ends[tid] = 0xFFFFFFFFu;
+    }
     __syncthreads();
     // keys [lo, hi] of the bins of either cut; none: an empty range
     uint32_t lo[2] = {0xFFFFFFFFu, 0xFFFFFFFFu}, hi[2] = {0u, 0u};
@@ -1321,8 +1360,7 @@ __global__ void __launch_bounds__(kSplitLanes) gather_kernel(SampleArgs a, int s
     if (goal.by_k) {
         cut.cross(false, goal.k, 0.0, 0, 0);
         const uint32_t bin = sh.bin;
-        lo[0] = cut.first_key(bin);
-        hi[0] = cut.last_key(bin);
+        cut.keys_of(bin, bin, &lo[0], &hi[0]);
         least = sh.above_w;
         most = least + sh.weight[bin];
         if (s == 0 && tid == 0) {
@@ -1336,14 +1374,14 @@ __global__ void __launch_bounds__(kSplitLanes) gather_kernel(SampleArgs a, int s
         // top-p's cut is between the goals that these bounds give (at least half a unit: a weight reaches it)
         const double g = goal.p * (double)least;
         cut.cross(true, 0, g < 0.5 ? 0.5 : g, 0, 0);
-        hi[1] = cut.last_key(sh.bin);
+        const uint32_t bin = sh.bin;
         if (s == 0 && tid == 0) w.above_w[1] = sh.above_w;
         __syncthreads();
         if (goal.by_k) {
             const double up = goal.p * (double)most;
             cut.cross(true, 0, up < 0.5 ? 0.5 : up, 0, 0);
         }
-        lo[1] = cut.first_key(sh.bin);
+        cut.keys_of(bin, sh.bin, &lo[1], &hi[1]);
         __syncthreads();
     }
     // sh.list and sh.list_w hold the two lists until they are copied
@@ -1351,7 +1389,7 @@ __global__ void __launch_bounds__(kSplitLanes) gather_kernel(SampleArgs a, int s
     const bool on[2] = {goal.by_k, goal.by_p};
     X low[2] = {to[0], to[1]}, high[2] = {from[0], from[1]};
     bool any[2] = {false, false};
-    cut.walk([&](const X (&v)[S::V], int first) {
+    cut.template walk<4>([&](const X (&v)[S::V], int first) {
 #pragma unroll
         for (int c = 0; c < 2; ++c) {
             if (!on[c]) continue;
@@ -1377,14 +1415,19 @@ __global__ void __launch_bounds__(kSplitLanes) gather_kernel(SampleArgs a, int s
         if (!__any(any[c])) continue;
         const uint32_t k0 = ~wave_max(any[c] ? ~S::key(low[c]) : 0u), k1 = wave_max(any[c] ? S::key(high[c]) : 0u);
         if ((tid & 63) == 0) {
-            atomicMin(&w.lo[c], k0);
-            atomicMax(&w.hi[c], k1);
+            atomicMin(&ends[c], k0);
+            atomicMax(&ends[2 + c], k1);
         }
     }
     __syncthreads();
-    if (tid < 2) {
+    if (tid < 2) {  // one set of the row's atomics a workgroup: they wait for each other
         w.found[tid][s] = listed[tid];
-        base[tid] = listed[tid] ? atomicAdd(&w.listed[tid], listed[tid]) : 0u;
+        base[tid] = 0u;
+        if (listed[tid]) {
+            base[tid] = atomicAdd(&w.listed[tid], listed[tid]);
+            atomicMin(&w.lo[tid], ends[tid]);
+            atomicMax(&w.hi[tid], ends[2 + tid]);
+        }
     }
     __syncthreads();
     for (int c = 0; c < 2; ++c) {
@@ -1451,7 +1494,7 @@ __global__ void __launch_bounds__(kSplitLanes) sum_kernel(SampleArgs a, int spli
 }
 
 template <int kType>
-__global__ void __launch_bounds__(kCutLanes) draw_kernel(SampleArgs a, int splits, const SplitRow* rows) {
+__global__ void __launch_bounds__(kCutLanes, 4) draw_kernel(SampleArgs a, int splits, const SplitRow* rows) {
     using S = Scores<kType>;
     __shared__ CutShared<kCutLanes> sh;
     const int64_t r = a.row0 + blockIdx.x;
@@ -1467,16 +1510,13 @@ __global__ void __launch_bounds__(kCutLanes) draw_kernel(SampleArgs a, int split
         cut_row(a, r, row, par, sh);
         return;
     }
-    // the draw takes kSplitLanes lanes: one for every region
-    if (threadIdx.x >= kSplitLanes) return;
-    static_assert(kMaxSplits * kSplitWaves <= kSplitLanes, "a lane for every region");
+    static_assert(kMaxSplits * kSplitWaves <= kCutLanes, "a lane for every region");
     Part* parts = reinterpret_cast<Part*>(sh.list);
     static_assert(sizeof(sh.list) >= sizeof(w.part), "the parts fit the list's room");
     const int regions = splits * kSplitWaves;
     if ((int)threadIdx.x < regions) parts[threadIdx.x] = w.part[threadIdx.x];
     __syncthreads();
-    draw_kept<kSplitLanes>(a, r, row, par, Kept<S>(w.last), goal, parts, regions,
-                           reinterpret_cast<PickShared<kSplitLanes>&>(sh.weight));
+    draw_kept<kCutLanes>(a, r, row, par, Kept<S>(w.last), goal, parts, regions, sh.pick);
 }
 
 // Workgroups a row without filters is split into: until the chip has two for every CU, with 4,096 entries
@@ -1488,12 +1528,12 @@ int splits_of(int32_t R, int32_t N) {
     return s < 1 ? 1 : (int)s;
 }
 
-// Workgroups a row with filters is split into, 4,096 entries or more to each; 0: one of kCutLanes lanes and a single
-// launch.  Splitting takes five launches, in which every split works out the row's cuts for itself, and pays while the
-// rows alone leave most of the chip idle: 16 rows of 131,072 entries 52 against 132 us, 64 of 65,536 as fast either way,
-// 256 of 32,768 93 against 49.
+// Workgroups a row with filters is split into, 4,096 entries or more to each; 0: one workgroup and a single launch.
+// Splitting takes five launches, in which every split works out the row's cuts for itself, and pays while the rows
+// alone leave most of the chip idle: 16 rows of 131,072 i32 with top-p 42 against 150 us, 64 of 32,768 41 against 48,
+// 256 of 131,072 162 against 181; but one of 16,384 27 against 22, 128 of 32,768 56 against 49.
 int cut_splits_of(int32_t R, int32_t N) {
-    if (N < 16384 || (int64_t)R * 1000 > N) return 0;
+    if (N < 24576 || (int64_t)R * 500 > N) return 0;
     int64_t s = 1024 / R, most = N / 4096;
     if (s > most) s = most;
     if (s > kMaxSplits) s = kMaxSplits;
