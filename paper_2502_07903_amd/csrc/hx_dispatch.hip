@@ -372,7 +372,8 @@ struct Demand {
             add = raw < 0 ? 0 : raw;
             fits = fits && raw >= 0 && held + add <= INT32_MAX;
             // 32-bit divisions: held + add is below 2^31 wherever the quotient counts
-            const uint32_t b = (uint32_t)bs, b0 = ((uint32_t)held + b - 1) / b, b1 = ((uint32_t)(held + add) + b - 1) / b;
+            const uint32_t b = (uint32_t)bs;
+            const uint32_t b0 = ((uint32_t)held + b - 1) / b, b1 = ((uint32_t)(held + add) + b - 1) / b;
             fits = fits && b1 <= (uint32_t)a.r.max_blocks;
             blocks = fits ? b1 - b0 : 0u;
         } else {
@@ -463,7 +464,7 @@ __global__ void __launch_bounds__(kLanes) kv_rows_kernel(KvArgs a, int fill) {
     }
     if (tid == 0) carry = 0;
     if (!kOne && kPlace) {
-        const u64 tokens = block_scan(tid < (int)blockIdx.x ? a.tokens[tid] : 0, wave_sum);  // at most kChunks <= kLanes
+        const u64 tokens = block_scan(tid < (int)blockIdx.x ? a.tokens[tid] : 0, wave_sum);  // kChunks <= kLanes
         if (tid == kLanes - 1) carry = tokens;
     }
     __syncthreads();
@@ -513,7 +514,8 @@ __global__ void __launch_bounds__(kLanes) kv_rows_kernel(KvArgs a, int fill) {
     }
     __syncthreads();
     if (tid < R) {
-        if (kOne) a.p.free_out[tid] = (int32_t)(kPlace ? free0[tid] - (int64_t)moved[tid] : free0[tid] + (int64_t)moved[tid]);
+        const int64_t by = (int64_t)moved[tid];
+        if (kOne) a.p.free_out[tid] = (int32_t)(kPlace ? free0[tid] - by : free0[tid] + by);
         else if (moved[tid]) atomicMax(&a.moved[tid], moved[tid]);
     }
     if (kPlace && kOne && fill) {

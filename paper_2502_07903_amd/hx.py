@@ -847,7 +847,8 @@ class Refiner:
     A round given one 64-bit draw (`draw`, int64 of one entry) takes over a child drawn from the
     children's flow values by `sampling` (hx_sample; temperature in milli-requests/s) instead of
     the best: a chain that may pass through worse placements, and so leave a local maximum.
-    `drawn` then holds the child taken; best still names the best child."""
+    `drawn` then holds the child taken; best still names the best child.  Parameters out of range
+    draw none (index -1), which leaves a parent without groups."""
     parent: DeviceProblem
     parent_ws: Workspace
     node_cls: object

@@ -81,6 +81,15 @@ def test_route_many(torch):
     check_route(torch, (70, 64, P * D + 50), [P, P], [D, D], flow, bits(rng, 4097), 1, lists=False)
 
 
+@pytest.mark.parametrize("P,D", [(3, 4), (100, 90)])
+def test_route_more_than_the_chunks(torch, P, D):
+    """More requests than 128 chunks of 1,024: a chunk is several of them."""
+    rng = np.random.default_rng([36, P])
+    flow = rng.integers(0, 9, (P * D, 1)).astype(np.int32)
+    say(f"route 150001 over {P} x {D}")
+    check_route(torch, (P, D, P * D), [P], [D], flow, bits(rng, 150001), 0)
+
+
 @pytest.mark.parametrize("n", [10, 3000])
 def test_route_nothing(torch, n):
     """No flow at all, no nodes on a side, counts past the arrays or negative: no routes, every list whole."""
@@ -194,6 +203,17 @@ def test_serving_steps(torch, rows, R, bs):
     m.place(np.zeros(rows), tag="nothing")
     m.release(np.ones(rows), tag="all")
     assert np.array_equal(m.h["free"], np.diff(m.h["base"]))
+
+
+def test_more_rows_than_the_chunks(torch):
+    rows, R = 140001, 3
+    rng = np.random.default_rng(46)
+    m = Memory(torch, [60000, 50000, 1], 16, rows, 4)
+    m.set(replica=rng.integers(-1, R, rows))
+    say("kv 140001 rows")
+    m.place(rng.integers(0, 30, rows), tag="prompts")
+    m.place(np.ones(rows), tag="tokens")
+    m.release(rng.random(rows) < 0.7)
 
 
 @pytest.mark.parametrize("rows", [3, 700, 4000])

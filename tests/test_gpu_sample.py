@@ -131,12 +131,12 @@ def test_ties(torch, name, N):
         check(torch, dev, bits(rng, R), par, f"ties {name} {N}")
 
 
+@pytest.mark.parametrize("N", [2050, 40001])
 @pytest.mark.parametrize("name", ("f32", "f16", "bf16"))
-def test_masks(torch, name):
+def test_masks(torch, name, N):
     dt = dtype(torch, name)
     low, big = torch.finfo(dt).min, torch.finfo(dt).max
     inf, nan = float("inf"), float("nan")
-    N = 2050
     x = torch.randn((12, N), generator=torch.Generator().manual_seed(5))
     x[0] = -inf
     x[1] = nan
@@ -180,7 +180,7 @@ def test_masked_int(torch):
         check(torch, dev, bits(rng, 6), par, "masked int32")
 
 
-@pytest.mark.parametrize("N", [50, 9000])
+@pytest.mark.parametrize("N", [50, 9000, 30001])
 def test_parameters(torch, N):
     """Every parameter at its edges; rows whose parameters are out of range draw nothing."""
     inf, nan = np.inf, np.nan
@@ -198,13 +198,14 @@ def test_parameters(torch, N):
     check(torch, x, bits(rng, R), par, "parameters")
 
 
+@pytest.mark.parametrize("N", [5003, 50021])
 @pytest.mark.parametrize("name", TYPES)
-def test_strides(torch, name):
+def test_strides(torch, name, N):
     """Padded rows, rows that start off a vector's alignment, one row read by all, overlapping rows; what lies between
     the rows is not read as a score."""
     rng = np.random.default_rng([17, TYPES.index(name)])
     dt = dtype(torch, name)
-    R, N = 9, 5003
+    R = 9
     big = torch.as_tensor(scores(rng, name, R, N + 13)).to("cuda").to(dt)
     big[:, N + 1:] = 30000  # larger than every score
     par = params(rng, R, "kp", name == "i32")
@@ -213,6 +214,44 @@ def test_strides(torch, name):
         say(f"sample strides {name} {tag}")
         check(torch, x, bits(rng, R), par, f"{tag} {name}")
         check(torch, x, bits(rng, R), params(rng, R, "", name == "i32"), f"{tag} {name}")
+
+
+@pytest.mark.parametrize("N", [700, 9000, 40000, 100003])
+def test_far_outliers(torch, N):
+    """One score far above the rest: all other scores fall into one bin of the distance from it, more than a list
+    holds, all different (float32) or in long runs (int32)."""
+    rng = np.random.default_rng([24, N])
+    R = 6
+    f = rng.normal(0, 1, (R, N)).astype(np.float32)
+    i = rng.integers(0, 500, (R, N)).astype(np.int32)
+    f[:, N // 3], i[:, N // 3] = 3e6, (1 << 31) - 1
+    f[5, :], i[5, :] = np.sort(f[5]), np.sort(i[5])
+    k = np.array([1, 2, 100, N // 2, N - 1, N], np.int32)
+    T = np.full(R, 1e6, np.float32)  # so that the rest has weight
+    p = np.array([0.1, 0.5, 0.9, 0.99, 0.999, 0.7], np.float32)
+    for name, x in (("f32", f), ("i32", i)):
+        dev = torch.as_tensor(x).to("cuda")
+        t = T * 1000 if name == "i32" else T
+        for par in (dict(T=t, k=k, p=None, q=None), dict(T=t, k=None, p=p, q=None), dict(T=t, k=k, p=p, q=None)):
+            say(f"sample outliers {name} N={N}")
+            check(torch, dev, bits(rng, R), par, f"outliers {name} {N}")
+
+
+@pytest.mark.parametrize("name", TYPES)
+@pytest.mark.parametrize("R,N", [(7, 3000), (7, 60000), (520, 9000)])
+def test_growing_rows(torch, name, R, N):
+    """Scores that grow along the row, at temperatures from far below their steps to far above: sums that start
+    relative to the first scores have to be scaled down, +inf at the end included."""
+    rng = np.random.default_rng([25, R, N, TYPES.index(name)])
+    x = np.sort(scores(rng, name, R, N, 5.0), axis=1)
+    if name != "i32":
+        x[R - 1, -1] = np.inf
+        x[R - 2, ::3] = -np.inf
+    dev = torch.as_tensor(x).to("cuda").to(dtype(torch, name))
+    T = np.resize(np.array([1e-30, 1e-4, 0.01, 0.1, 1.0, 3.0, 1e20], np.float32), R)
+    T = T * 1000 if name == "i32" else T
+    say(f"sample growing {name} {R} x {N}")
+    check(torch, dev, bits(rng, R), dict(T=T, k=None, p=None, q=None), f"growing {name}")
 
 
 def test_offsets_past_32_bits(torch):
