@@ -133,6 +133,7 @@ EXPORTS = ("hx_validate", "hx_cost_eval", "hx_cost_eval_static", "hx_static_scra
            "hx_profile", "hx_profile_read", "hx_kernel_name", "hx_strerror", "hx_last_error",
            "hx_abi_version")
 HX_KERNELS = 18
+HX_SCORING_KERNELS = 14  # the first ones: scoring, refinement and partition
 
 _lib = None
 
@@ -210,13 +211,15 @@ def profile(enable: bool) -> None:
 
 
 def profile_read() -> Dict[str, Tuple[float, int]]:
-    """{kernel name: (total ms, launches)} since the last profile() call; clears the records."""
+    """{kernel name: (total ms, launches)} since the last profile() call; clears the records.  The kernels of scoring,
+    refinement and partition are always named, the draw and dispatch calls where they were made."""
     ms = (C.c_double * HX_KERNELS)()
     n = (C.c_int32 * HX_KERNELS)()
     rc = lib().hx_profile_read(C.cast(ms, C.c_void_p), C.cast(n, C.c_void_p), HX_KERNELS)
     if rc < 0:
         _check(rc, "hx_profile_read")
-    return {lib().hx_kernel_name(k).decode(): (float(ms[k]), int(n[k])) for k in range(HX_KERNELS)}
+    return {lib().hx_kernel_name(k).decode(): (float(ms[k]), int(n[k])) for k in range(HX_KERNELS)
+            if k < HX_SCORING_KERNELS or n[k] > 0}
 
 
 def strerror(code: int) -> str:

@@ -132,3 +132,18 @@ def test_dispatcher_refuses(torch):
     for bad in ((0, 100, 100, 16), (8, 0, 100, 16), (8, 100, 0, 16), (8, 100, 100, 0)):
         with pytest.raises(ValueError):
             hx.Dispatcher.create(dp, 0, *bad)
+
+
+def test_profile_names_the_calls_made(torch):
+    dp = hx.DeviceProblem.upload(I.make_problem(1, n_cand=20))
+    hx.profile(True)
+    disp = hx.Dispatcher.create(dp, 0, 8, 100, 100)
+    rng = np.random.default_rng(53)
+    disp.admit(draws_of(torch, rng, 8)[1], torch.full((8,), 9, dtype=torch.int32, device="cuda"))
+    prof = hx.profile_read()
+    assert {k: prof[k][1] for k in ("route", "place", "release")} == dict(route=1, place=1, release=1)
+    assert all(prof[k][0] > 0.0 for k in ("route", "place", "release")) and "sample" not in prof
+    hx.sample(torch.zeros((2, 9), device="cuda"), draws_of(torch, rng, 2)[1], hx.SampleBuffers.empty(2, 9))
+    prof = hx.profile_read()
+    hx.profile(False)
+    assert prof["sample"][1] == 1 and prof["sample"][0] > 0.0 and "route" not in prof
