@@ -588,6 +588,8 @@ __device__ void finish_row(const SampleArgs& a, int64_t r, const Row<S>& row, co
 }
 
 // A row's split s of `splits`: workgroup r * splits + s.  With one split the row ends here.
+// Bound by the exponentials' binary64 operations, 27 vector instructions an entry in all: 1,024 rows of 131,072 bf16
+// 112 us a call, 2.4 TB/s, of which reading the 268 MB once is 52 us; a row of 256 i32 4.4 us, the launch.
 template <int kType>
 __global__ void __launch_bounds__(kAllLanes) all_kernel(SampleArgs a, int splits, Part* parts) {
     using S = Scores<kType>;
@@ -1233,6 +1235,9 @@ __device__ void cut_row(const SampleArgs& a, int64_t r, const Row<S>& row, const
     draw_kept<kCutLanes>(a, r, row, par, kept, goal, sh.part, kCutWaves, sh.pick);
 }
 
+// 256 rows of 50,257 f16 with top-p and min-p: 77 us, of which a row takes 4 for its extent, 22 for the bins' weights
+// (an exponential and two LDS atomics an entry), 7 to 25 for the cut, 8 for the kept entries' sums and 4 for the draw.
+// The later passes find the row in the caches; every pass ends in a barrier that waits for the slowest wavefront.
 template <int kType>
 __global__ void __launch_bounds__(kCutLanes, 4) cut_kernel(SampleArgs a) {  // four wavefronts a SIMD: 128 registers
     using S = Scores<kType>;
@@ -1250,6 +1255,8 @@ __global__ void __launch_bounds__(kCutLanes, 4) cut_kernel(SampleArgs a) {  // f
 //   gather_kernel  the entries of the bins in which the cuts fall, into the row's lists
 //   sum_kernel     the cuts, from the lists; weight and number of the regions' kept entries
 //   draw_kernel    a workgroup per row: the draw
+// 16 rows of 131,072 i32 with top-p: 4.5, 8.5, 10.5, 13.5 and 6 us.  Each launch is bound by its chain: the first
+// loads, the row's state from the other workgroups, one pass over 4,096 entries or more, the reduction.
 // A bin with more entries than a list holds is of one score as a rule (16-bit scores): the cut is then a number of
 // them, and the split in which the last one is finds it.  A row with a longer list of different scores is cut as a
 // whole by draw_kernel.
@@ -1528,33 +1535,31 @@ int splits_of(int32_t R, int32_t N) {
     return s < 1 ? 1 : (int)s;
 }
 
+constexpr int32_t kSplitRows = 192;  // of more rows none is split
+
 // Workgroups a row with filters is split into, 4,096 entries or more to each; 0: one workgroup and a single launch.
 // Splitting takes five launches, in which every split works out the row's cuts for itself, and pays while the rows
 // alone leave most of the chip idle: 16 rows of 131,072 i32 with top-p 42 against 150 us, 64 of 32,768 41 against 48,
-// 256 of 131,072 162 against 181; but one of 16,384 27 against 22, 128 of 32,768 56 against 49.
+// 192 of 131,072 f32 with top-k and top-p 129 against 162, one of 8,388,608 124 against 6,586; but one of 16,384 27
+// against 22, 128 of 32,768 56 against 49, 260 of 131,072 215 against 192, 512 of 262,144 1,297 against 572.  Where a
+// row's lists overflow, which rows of a million float scores can, it costs a quarter more: 64 rows 1,681 against 1,452.
 int cut_splits_of(int32_t R, int32_t N) {
-    if (N < 24576 || (int64_t)R * 500 > N) return 0;
+    if (N < 24576 || R > kSplitRows || (int64_t)R * 500 > N) return 0;
     int64_t s = 1024 / R, most = N / 4096;
     if (s > most) s = most;
-    if (s > kMaxSplits) s = kMaxSplits;
-    return s < 1 ? 1 : (int)s;
+    return (int)(s < kMaxSplits ? s : kMaxSplits);
 }
 
-constexpr int32_t kRowsPerLaunch = 1 << 20;  // a grid has fewer than 2^32 lanes
-constexpr int32_t kSplitRows = 256;          // rows of SplitRow that the workspace has
+constexpr int32_t kRowsPerLaunch = 1 << 20;  // a grid has fewer than 2^32 lanes; split rows are far fewer
 
-size_t cut_workspace(int32_t R, int32_t N) {
-    return cut_splits_of(R, N) ? sizeof(SplitRow) * (R < kSplitRows ? R : kSplitRows) : 0;
-}
+size_t cut_workspace(int32_t R, int32_t N) { return cut_splits_of(R, N) ? sizeof(SplitRow) * R : 0; }
 
 template <int kType>
 hipError_t launch(SampleArgs a, void* workspace, hipStream_t s) {
     const bool filters = a.top_k || a.top_p || a.min_p;
     const int splits = filters ? cut_splits_of(a.R, a.N) : splits_of(a.R, a.N);
-    // several launches share the workspace: one after the other on the stream
-    const int32_t per = filters && splits ? kSplitRows : kRowsPerLaunch;
-    for (int64_t r0 = 0; r0 < a.R; r0 += per) {
-        const unsigned rows = (unsigned)(a.R - r0 < per ? a.R - r0 : per);
+    for (int64_t r0 = 0; r0 < a.R; r0 += kRowsPerLaunch) {
+        const unsigned rows = (unsigned)(a.R - r0 < kRowsPerLaunch ? a.R - r0 : kRowsPerLaunch);
         a.row0 = r0;
         if (!filters) {
             Part* parts = static_cast<Part*>(workspace);  // more splits than one: few rows

@@ -109,6 +109,17 @@ def test_many_rows(torch, name, R, N):
         check(torch, x, bits(rng, R), params(rng, R, which, name == "i32"), f"{name} {R}x{N} {which}")
 
 
+@pytest.mark.parametrize("name", ["i32", "bf16"])
+@pytest.mark.parametrize("R", [192, 193])
+def test_most_split_rows(torch, name, R):
+    """The most rows that are split over workgroups where they are long enough, and one more."""
+    N = 98304
+    rng = np.random.default_rng([21, R, TYPES.index(name)])
+    say(f"sample {name} {R} x {N}")
+    x = torch.as_tensor(scores(rng, name, R, N)).to("cuda").to(dtype(torch, name))
+    check(torch, x, bits(rng, R), params(rng, R, "kpq", name == "i32"), f"{name} {R}x{N}")
+
+
 @pytest.mark.parametrize("name", TYPES)
 @pytest.mark.parametrize("N", [37, 3000, 70000])
 def test_ties(torch, name, N):
