@@ -763,25 +763,29 @@ class Dispatcher:
             raise ValueError("requests are dispatched to replicas: granularity 0")
         if n_rows < 1 or max_tokens < 1 or max_slots < 1 or block_size < 1:
             raise ValueError("rows, tokens, slots and the block size must be at least 1")
-        one = dp.with_candidates(dp.tensors["assign"][:, cand:cand + 1].clone(),
-                                 dp.tensors["role"][:, cand:cand + 1].clone())
-        ws = Workspace.for_problem(one, flows=True, device=device)
-        score(one, ws, stream)
-        (torch.cuda.current_stream() if stream is None else stream).synchronize()
-        n_d = int(ws.net.n_d[0])
-        width = -(-max_tokens // block_size)
-        mean = -(-int(np.ceil(dp.workload.s_in + dp.workload.s_out)) // block_size)
-        bmax = ws.cost.bmax[:, 0].cpu().numpy().astype(np.int64)
-        blocks = np.zeros(ws.net.dims[1], np.int64)
-        blocks[:n_d] = np.minimum(bmax[ws.net.d_slot[:n_d, 0].cpu().numpy()] * mean, n_rows * width)
-        z = lambda n, dt, v=0: torch.full((n,), v, dtype=dt, device=device)
-        routes = RouteBuffers.empty(ws.net.dims, n_rows, device)
-        rows = KvRows.empty(n_rows, width, device)
-        rows.replica = routes.decode
-        rows.replica.fill_(-1)
-        return cls(one, ws, routes, KvPool.create(blocks, block_size, device), rows, z(n_rows + 1, torch.int64),
-                   z(max_slots, torch.int64), z(n_rows, torch.uint8), kv_workspace(n_rows, len(blocks), device),
-                   z(n_rows, torch.int32, 1), z(n_rows, torch.uint8, 1))
+        if not 0 <= cand < dp.cand.n_cand:
+            raise ValueError(f"column {cand} of a batch of {dp.cand.n_cand}")
+        if stream is not None:
+            stream.wait_stream(torch.cuda.current_stream())  # what dp's tensors still wait for
+        with torch.cuda.stream(stream):
+            one = dp.with_candidates(dp.tensors["assign"][:, cand:cand + 1].clone(),
+                                     dp.tensors["role"][:, cand:cand + 1].clone())
+            ws = Workspace.for_problem(one, flows=True, device=device)
+            score(one, ws, stream)
+            n_d = int(ws.net.n_d[0])
+            width = -(-max_tokens // block_size)
+            mean = -(-int(np.ceil(dp.workload.s_in + dp.workload.s_out)) // block_size)
+            bmax = ws.cost.bmax[:, 0].cpu().numpy().astype(np.int64)
+            blocks = np.zeros(ws.net.dims[1], np.int64)
+            blocks[:n_d] = np.minimum(bmax[ws.net.d_slot[:n_d, 0].cpu().numpy()] * mean, n_rows * width)
+            z = lambda n, dt, v=0: torch.full((n,), v, dtype=dt, device=device)
+            routes = RouteBuffers.empty(ws.net.dims, n_rows, device)
+            rows = KvRows.empty(n_rows, width, device)
+            rows.replica = routes.decode
+            rows.replica.fill_(-1)
+            return cls(one, ws, routes, KvPool.create(blocks, block_size, device), rows, z(n_rows + 1, torch.int64),
+                       z(max_slots, torch.int64), z(n_rows, torch.uint8), kv_workspace(n_rows, len(blocks), device),
+                       z(n_rows, torch.int32, 1), z(n_rows, torch.uint8, 1))
 
     def admit(self, rnd, prompt, stream=None) -> None:
         """A request in every row, over whatever the rows held: routed by its draw (rnd, int64 bit patterns), its

@@ -147,3 +147,40 @@ def test_profile_names_the_calls_made(torch):
     prof = hx.profile_read()
     hx.profile(False)
     assert prof["sample"][1] == 1 and prof["sample"][0] > 0.0 and "route" not in prof
+
+
+def test_dispatcher_on_its_own_stream(torch):
+    """Created and used on a stream that is not the current one, while the current one is still busy with its batch."""
+    prob = I.make_problem(1, n_cand=64)
+    dp = hx.DeviceProblem.upload(prob)
+    want = hx.Dispatcher.create(dp, 5, 40, 64, 40 * 64)
+    late = {k: dp.tensors[k].clone() for k in ("assign", "role")}
+    busy = torch.zeros(1 << 26, device="cuda")
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    zero = {k: torch.zeros_like(v) for k, v in late.items()}
+    moved = dp.with_candidates(zero["assign"], zero["role"])
+    for _ in range(20):
+        busy.add_(1.0)
+    for k, v in late.items():
+        zero[k].copy_(v)
+    got = hx.Dispatcher.create(moved, 5, 40, 64, 40 * 64, stream=side)
+    rnd = torch.arange(40, device="cuda", dtype=torch.int64) * 0x0123456789ABCDEF
+    prompt = torch.full((40,), 3, dtype=torch.int32, device="cuda")
+    torch.cuda.synchronize()
+    want.admit(rnd, prompt)
+    want.step()
+    got.admit(rnd, prompt, side)
+    got.step(stream=side)
+    torch.cuda.synchronize()
+    for a, b in ((want.rows.held, got.rows.held), (want.rows.table, got.rows.table), (want.slots, got.slots),
+                 (want.pool.free_count, got.pool.free_count), (want.routes.decode, got.routes.decode)):
+        assert torch.equal(a, b)
+    assert int(got.rows.held.sum()) > 0
+
+
+@pytest.mark.parametrize("cand", [-1, 2])
+def test_dispatcher_refuses_columns(torch, cand):
+    dp = hx.DeviceProblem.upload(I.make_problem(1, n_cand=2))
+    with pytest.raises(ValueError):
+        hx.Dispatcher.create(dp, cand, 4, 16, 64)
