@@ -286,6 +286,28 @@ def test_long_row(torch, N):
             check(torch, x, bits(rng, 2), params(rng, 2, which, name == "i32"), f"long {name}")
 
 
+@pytest.mark.parametrize("name", ["i32", "bf16"])
+def test_longest_row(torch, name):
+    """Rows of HX_MAX_COLS equal scores, whose draws are known without sorting: both rows are the same one."""
+    N = 1 << 30
+    x = torch.full((1, N), 3, dtype=dtype(torch, name), device="cuda").expand(2, N)
+    draws = np.array([0xFFFFFFFFFFFFFFFF, 0x6A09E667F3BCC908], np.uint64)
+    out = hx.SampleBuffers.empty(2, N)
+    T = np.full(2, 2.0, np.float32)
+    for par, kept in ((dict(T=T, k=None, p=None, q=None), [N, N]),
+                      (dict(T=T, k=np.array([(1 << 29) + 1, 1], np.int32), p=None, q=None), [(1 << 29) + 1, 1]),
+                      (dict(T=T, k=None, p=np.array([0.25, 0.75], np.float32), q=None), [1 << 28, 3 << 28]),
+                      (dict(T=T, k=np.full(2, 1000, np.int32), p=T / 4, q=T / 4), [500, 500])):
+        say(f"sample {name} 2 x {N} {kept}")
+        hx.sample(x, device_draws(torch, draws), out, device_params(torch, par))
+        torch.cuda.synchronize()
+        # the first entry past u S is the whole part of u S: exact, since neither product is near a whole number
+        want = [(int(d) >> 11) * k >> 53 for d, k in zip(draws, kept)]
+        assert out.kept.tolist() == kept and out.pick.tolist() == want
+        err = np.abs(out.logp.cpu().numpy() + np.log(np.array(kept, np.float64)))
+        assert (err <= np.log(np.array(kept, np.float64)) * 2.0 ** -24 * 1.001 + 1e-11).all()
+
+
 def test_follows_the_weights(torch):
     """The draws of one row with its probabilities: 40,000 draws of the same scores, frequencies within five standard
     deviations of the kept probabilities."""
