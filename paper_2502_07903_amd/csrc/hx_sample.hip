@@ -941,7 +941,7 @@ struct Cutter {
     }
 
     // The cut among the listed entries: split by the bits of their places until at most kRank are left, which
-    // are ranked.
+    // are ranked.  Sums of whole numbers cross in every round; one that did not would leave in_bin 0 and end the loop.
     __device__ u64 cut_list(uint32_t number, bool by_weight, u64 want, double goal, u64 above_c, u64 above_w,
                             u64* up_to) {
         const int tid = threadIdx.x;
@@ -954,6 +954,7 @@ struct Cutter {
                 sh.hi64 = 0;
             }
             clear_bins();
+            if (tid == 0) sh.in_bin = 0;
             u64 least = ~(u64)0, most = 0;
             for (uint32_t i = tid; i < number; i += kLanes) {
                 const u64 p = sh.list[i];
@@ -984,8 +985,8 @@ struct Cutter {
             above_c = sh.above_c;
             above_w = sh.above_w;
             lo += (u64)sh.bin << shift;
-            const u64 end = lo + (((u64)1 << shift) - 1);
-            hi = end < hi ? end : hi;
+            const u64 span = ((u64)1 << shift) - 1;  // lo + span can pass 2^64: the lowest int32 scores' places end there
+            hi = hi - lo > span ? lo + span : hi;
         }
         // at most kRank entries: each against all
         if (tid == 0) sh.listed = 0;
@@ -994,10 +995,10 @@ struct Cutter {
             const u64 p = sh.list[i];
             if (p < lo || p > hi) continue;
             const uint32_t at = atomicAdd(&sh.listed, 1u);
-            sh.some[at] = ulonglong2{p, sh.list_w[i]};
+            if (at < kRank) sh.some[at] = ulonglong2{p, sh.list_w[i]};
         }
         __syncthreads();
-        const uint32_t left = sh.listed;
+        const uint32_t left = sh.listed < kRank ? sh.listed : kRank;
         if ((uint32_t)tid < left) {
             const u64 p = sh.some[tid].x, w = sh.some[tid].y;
             u64 before = above_c, before_w = above_w;

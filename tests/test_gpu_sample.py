@@ -404,3 +404,45 @@ def test_refuses(torch):
     out.workspace = out.workspace[:0]
     with pytest.raises(hx.HxError):
         hx.sample(x, d, out)
+
+
+LOW = O.I32_MIN + 1  # the lowest int32 score
+
+
+def low_rows(kind, N):
+    """Rows whose cuts fall among the type's lowest scores, whose places end where 64 bits do."""
+    rng = np.random.default_rng([61, N])
+    if kind == "uniform":
+        return rng.integers(LOW, 1 << 31, (6, N)).astype(np.int32)
+    x = np.concatenate([[(1 << 31) - 1, LOW + 4000000], np.arange(LOW, LOW + 500),
+                        rng.integers(LOW + 8000000, 1 << 31, N - 502)])
+    return np.stack([rng.permutation(x) for _ in range(6)]).astype(np.int32)
+
+
+@pytest.mark.parametrize("kind", ["uniform", "lowest"])
+@pytest.mark.parametrize("N", [502, 2000, 30000, 131072])
+def test_cuts_among_the_lowest_ints(torch, kind, N):
+    """By one workgroup and split over several: top-k's and top-p's cuts at every depth of the last bin's list."""
+    x = torch.as_tensor(low_rows(kind, N)).to("cuda")
+    rng = np.random.default_rng([62, N])
+    k = np.array([N - 1, N - 2, N - 100, N - 300, N - 490, N], np.int32)
+    ones = np.ones(6, np.float32)
+    p = np.array([0.5, 0.9, 0.99, 0.999, 0.9995, 0.9999], np.float32)
+    for T in (1000.0, 3e8, 3e9):
+        for par in (dict(T=ones * T, k=k, p=None, q=None), dict(T=ones * T, k=k, p=ones * 0.5, q=None),
+                    dict(T=ones * T, k=None, p=p, q=None), dict(T=ones * T, k=k, p=p, q=ones * 1e-5)):
+            say(f"sample lowest int32 {kind} N={N} T={T} {[n for n in 'kpq' if par[n] is not None]}")
+            check(torch, x, bits(rng, 6), par, f"lowest int32 {kind} {N}")
+
+
+def test_the_lowest_ints_after_one_far_above(torch):
+    """One bin with 500 scores next to each other at the type's end, one 4 million above them, one at its other end."""
+    row = np.concatenate([[(1 << 31) - 1, LOW - 1 + 4000000], np.arange(LOW, LOW + 500)]).astype(np.int32)
+    k = np.array([1, 2, 3, 100, 300, 400, 501, 502], np.int32)
+    x = torch.as_tensor(np.tile(row, (len(k), 1))).to("cuda")
+    T = np.full(len(k), 2e9, np.float32)
+    rng = np.random.default_rng(63)
+    for par in (dict(T=None, k=k, p=None, q=None), dict(T=T, k=k, p=None, q=None),
+                dict(T=T, k=None, p=(0.999 * k / 502).astype(np.float32), q=None)):
+        say(f"sample lowest int32 after one {[n for n in 'Tkpq' if par[n] is not None]}")
+        check(torch, x, bits(rng, len(k)), par, "lowest int32 after one")
