@@ -12,11 +12,11 @@
 //
 // With filters (cut_kernel, a workgroup per row): all three keep a prefix of the order (descending score,
 // ascending index), so the kept set is everything up to one entry's place in it.  That entry is found by
-// counting, for top-k, and by adding whole-number weights, for top-p (64-bit sums: no order of addition
-// changes them), in 1,024 bins of the distance from m.  The entries of the bin in which the cut falls, if
-// at most kList, go to a list in LDS, which is split by the bits of their places until a wavefront can rank
-// the rest; a longer bin is split again by the keys' bits over the row.  min-p's bound is a search over the
-// keys.
+// counting, for top-k, and by adding whole-number weights, for top-p (no order of addition changes their
+// sums, and each bin has a unit of its own, as fine as 64 bits allow for weights of its size), in 1,024 bins
+// of the distance from m.  The entries of the bin in which the cut falls, if at most kList, go to a list in
+// LDS, which is split by the bits of their places until a wavefront can rank the rest; a longer bin is split
+// again by the keys' bits over the row.  min-p's bound is a search over the keys.
 #include <float.h>
 #include <math.h>
 
@@ -28,6 +28,7 @@ namespace hx {
 namespace {
 
 using u64 = unsigned long long;
+using u128 = unsigned __int128;
 
 // ------------------------------------------------------------------ scores
 
@@ -310,6 +311,16 @@ __device__ __forceinline__ A last_lane(A v) {
     __builtin_memcpy(&v, w, sizeof(A));
     return v;
 }
+// A value that all lanes have, to scalar registers.
+template <class A>
+__device__ __forceinline__ A scalar(A v) {
+    int w[sizeof(A) / 4];
+    __builtin_memcpy(w, &v, sizeof(A));
+#pragma unroll
+    for (int k = 0; k < (int)sizeof(A) / 4; ++k) w[k] = __builtin_amdgcn_readfirstlane(w[k]);
+    __builtin_memcpy(&v, w, sizeof(A));
+    return v;
+}
 template <class A>
 __device__ __forceinline__ A wave_scan(A v) {  // inclusive
     v += move<0x111, 0xf>(v, A(0));
@@ -323,6 +334,21 @@ __device__ __forceinline__ A wave_scan(A v) {  // inclusive
 template <class A>
 __device__ __forceinline__ A wave_sum(A v) {
     return last_lane(wave_scan(v));
+}
+// The sum of the first `number` words of x, at most eight, each lane of a wavefront reading one.
+template <class A>
+__device__ __forceinline__ A sum_of_first(const A* x, int number) {
+    const int lane = threadIdx.x & 63;
+    A v = lane < number ? x[lane] : A(0);
+    v += move<0x111, 0xf>(v, A(0));
+    v += move<0x112, 0xf>(v, A(0));
+    v += move<0x114, 0xf>(v, A(0));
+    int w[sizeof(A) / 4];
+    __builtin_memcpy(w, &v, sizeof(A));
+#pragma unroll
+    for (int k = 0; k < (int)sizeof(A) / 4; ++k) w[k] = __builtin_amdgcn_readlane(w[k], 7);
+    __builtin_memcpy(&v, w, sizeof(A));
+    return v;
 }
 template <class A>
 __device__ __forceinline__ A wave_max(A v) {
@@ -667,12 +693,30 @@ struct CutShared {
     u64 weight[kBins];
     u64 list[kLists ? kList : 1], list_w[kLists ? kList : 1];
     ulonglong2 some[kRank];  // place, weight
-    u64 wave_c[kWaves], wave_w[kWaves];
-    u64 above_c, above_w, in_bin, found, found_w, lo64, hi64;
+    u64 wave_c[kWaves], wave_w[kWaves], wave_h[kWaves];
+    u128 above_w;
+    u64 above_c, in_bin, found, found_w, lo64, hi64;
     uint32_t bin, listed, lo, hi;
     Part part[kWaves];
     PickShared<kLanes> pick;
 };
+
+// Weights of several bins are whole numbers of up to 97 bits: those of a bin shifted to the last bin's unit.  Sums go
+// over lanes in two parts, of 48 bits and the rest.
+constexpr int kPart = 48;
+__device__ __forceinline__ u64 low_part(u128 v) { return (u64)v & (((u64)1 << kPart) - 1); }
+__device__ __forceinline__ u64 high_part(u128 v) { return (u64)(v >> kPart); }
+// The same of w << shift: w below 2^63, shift at most 48.
+__device__ __forceinline__ u64 low_part(u64 w, int shift) { return (w << shift) & (((u64)1 << kPart) - 1); }
+__device__ __forceinline__ u64 high_part(u64 w, int shift) { return w >> (kPart - shift); }
+__device__ __forceinline__ u128 joined(u64 low, u64 high) { return ((u128)high << kPart) + low; }
+// The least whole number, from 1 up, that is at least p times v (both rounded to binary64).
+__device__ __forceinline__ u128 share_of(double p, u128 v) {
+    const double x = ceil(p * ((double)high_part(v) * 0x1p48 + (double)low_part(v)));
+    const double high = trunc(x * 0x1p-48);
+    const u128 r = joined((u64)(x - high * 0x1p48), (u64)high);
+    return r ? r : 1;
+}
 
 // A row's extent: its largest and smallest score's keys and the number of its entries.
 struct Extent {
@@ -692,7 +736,11 @@ struct Goal {
     uint32_t top_key;
     Exponent ex;
     float bins_per;  // distance bins per unit of score
-    int unit;        // whole-number weights are w 2^unit, rounded: the sums stay below 2^62
+    // A weight of bin b is a whole number of 2^-(unit + more), more = b finer / 2^20 rounded up.  No weight of the bin
+    // is above 2^-(b finer / 2^20) (finer is a thousandth less than the bins' width has it, for the roundings of a
+    // distance): the whole numbers are at most 2^(unit + 1), their sums below 2^62, and down to the last bin, in which
+    // more is 35 at most, each is off by 2^-(unit + 1) of itself, or 3% more.
+    int unit, finer;
     __device__ __forceinline__ Goal(const Parameters& par, const Extent& e, int n) {
         nothing = e.count == 0 || par.bad;
         one = par.T == 0.0f || par.q > 1.0f || par.p <= 0.0f || par.k == 1;
@@ -707,9 +755,13 @@ struct Goal {
         // weights past 24 T below the top add less than 4e-11 each: their bins need no width of their own; a count
         // alone goes by the scores' range
         const float reach = 24.0f * par.T, spread = S::below(top, S::value(e.low));
-        bins_per = (float)(kBins - 1) / (par.p < 1.0f && reach < spread ? reach : spread);
+        const float range = par.p < 1.0f && reach < spread ? reach : spread;
+        bins_per = (float)(kBins - 1) / range;
+        // range / T is at most 24; a range so short that bins_per is infinite has no bins but the first and the last
+        const float bits_in_bins = fminf(range / par.T, 24.0f) * 1.44125f;
+        finer = by_p && bins_per <= FLT_MAX ? (int)(bits_in_bins * (1048576.0f / (kBins - 1))) : 0;
         const int bits = n > 1 ? 32 - __clz(n - 1) : 0;
-        unit = bits < 11 ? 51 : 62 - bits;
+        unit = bits < 11 ? 50 : 61 - bits;
     }
     // The last place whose weight is at least min-p; every lane of a wavefront calls it.
     __device__ __forceinline__ u64 last_by_weight() const {
@@ -726,27 +778,33 @@ template <int kLanes, class S, bool kLists = true>
 struct Cutter {
     using X = typename S::X;
     static constexpr int kWaves = kLanes / 64, kOwn = kBins / kLanes;  // bins of a lane
+    static_assert(kWaves <= 8, "sum_of_first");
     const Row<S>& row;
     Region mine;  // this wavefront's
     const Exponent& ex;
     X top;
     uint32_t top_key;
     float bins_per;
-    int unit;
+    int finer, first_one;
     bool weights;  // top-p is on
     bool filled;   // the bins hold the row's distances
     CutShared<kLanes, kLists>& sh;
     __device__ __forceinline__ Cutter(const Row<S>& r, const Region& g, const Goal<S>& goal,
                                       CutShared<kLanes, kLists>& shared)
-        : row(r), mine(g), ex(goal.ex), top(goal.top), top_key(goal.top_key), bins_per(goal.bins_per), unit(goal.unit),
-          weights(goal.by_p), filled(false), sh(shared) {}
+        : row(r), mine(g), ex(goal.ex), top(goal.top), top_key(goal.top_key), bins_per(goal.bins_per),
+          finer(goal.finer), first_one((1075 - goal.unit) << 20), weights(goal.by_p), filled(false), sh(shared) {}
 
-    // w 2^unit, rounded, is what adding 2^(52 - unit) leaves in the low bits (unit <= 51, w <= 1).
-    __device__ __forceinline__ u64 fixed(double w) const {
-        const double one = __longlong_as_double((long long)(1075 - unit) << 52);
-        return (u64)__double_as_longlong(w + one) - (u64)__double_as_longlong(one);
+    // Upper half of 2^(52 - u), 2^-u bin b's unit: what stays of its low bits after adding w is w 2^u, rounded.
+    __device__ __forceinline__ int one_of(uint32_t b) const {
+        return (__mul24((int)b, -finer) + first_one) & 0x7FF00000;
     }
-    __device__ __forceinline__ u64 fixed_of(X v) const { return weights ? fixed(ex.weight(v)) : 0; }
+    // How many bits the last bin's unit is finer.
+    __device__ __forceinline__ int shift_of(uint32_t b) const { return (one_of(b) - one_of(kBins - 1)) >> 20; }
+    __device__ __forceinline__ u64 fixed(double w, uint32_t b) const {
+        const int one = one_of(b);
+        return (u64)__double_as_longlong(w + __hiloint2double(one, 0)) - ((u64)(uint32_t)one << 32);
+    }
+    __device__ __forceinline__ u64 fixed_of(X v, uint32_t b) const { return weights ? fixed(ex.weight(v), b) : 0; }
     // Distance bins: equal scores share one, and a lower score is never in an earlier one.  NaN (inf - inf, or the
     // top itself where bins_per is infinite) goes to the first bin, what is past the range to the last.
     __device__ __forceinline__ uint32_t bin_of(X v) const {
@@ -801,11 +859,12 @@ struct Cutter {
 #pragma unroll
                 for (int e = 0; e < S::V; ++e) {
                     const uint32_t b = bin_of(v[e]);
+                    const u64 f = fixed(w[e], b);
                     if (b == kBins - 1) {
-                        far_w += fixed(w[e]);
+                        far_w += f;
                         ++far;
                     } else {
-                        atomicAdd(&sh.weight[b], fixed(w[e]));
+                        atomicAdd(&sh.weight[b], f);
                         if (counts) atomicAdd(&sh.count[b], 1u);
                     }
                 }
@@ -830,58 +889,66 @@ struct Cutter {
         __syncthreads();
     }
 
-    __device__ u64 total_weight() {
-        u64 w = 0;
-#pragma unroll
-        for (int i = 0; i < kOwn; ++i) w += sh.weight[threadIdx.x + i * kLanes];
-        w = wave_sum(w);
-        if ((threadIdx.x & 63) == 0) sh.wave_w[wave_index()] = w;
-        __syncthreads();
-        w = 0;
-        for (int k = 0; k < kWaves; ++k) w += sh.wave_w[k];
-        __syncthreads();
-        return w;
-    }
-
-    // The bin, from 0 up, in which the count passes want or the weight reaches goal; above_c and above_w are those of
-    // what precedes the bins.  Leaves bin, in_bin, above_c and above_w in LDS.
-    __device__ void cross(bool by_weight, u64 want, double goal, u64 above_c, u64 above_w) {
+    // The bin, from 0 up, in which the count reaches want or the weight goal; above_c and above_w are those of what
+    // precedes the bins.  Leaves bin, in_bin, above_c and above_w (with kFar of the distance bins, each shifted by its
+    // own; otherwise of 64 bits, in one bin's unit) in LDS.  Returns goal: with p, its share of all distance bins'
+    // weight.
+    template <bool kFar>
+    __device__ u128 cross(bool by_weight, u64 want, u128 goal, u64 above_c, u64 above_w, double p = 0.0) {
         const int wave = wave_index(), lane = threadIdx.x & 63;
-        u64 c[kOwn], w[kOwn], sum_c = 0, sum_w = 0;
+        uint32_t c[kOwn], sum_c = 0;
+        u64 w[kOwn], high[kOwn], sum_w = 0, sum_h = 0;
 #pragma unroll
         for (int i = 0; i < kOwn; ++i) {
-            c[i] = sh.count[kOwn * threadIdx.x + i];
-            w[i] = weights ? sh.weight[kOwn * threadIdx.x + i] : 0;
+            const uint32_t b = kOwn * threadIdx.x + i;
+            c[i] = sh.count[b];
+            w[i] = weights ? sh.weight[b] : 0;
+            high[i] = 0;
+            if (kFar) {
+                const int shift = shift_of(b);
+                high[i] = high_part(w[i], shift);
+                w[i] = low_part(w[i], shift);
+            }
             sum_c += c[i];
             sum_w += w[i];
+            sum_h += high[i];
         }
-        const u64 sc = wave_scan(sum_c), sw = weights ? wave_scan(sum_w) : 0;
+        const uint32_t sc = wave_scan(sum_c);
+        const u64 sw = weights ? wave_scan(sum_w) : 0, su = kFar && weights ? wave_scan(sum_h) : 0;
         if (lane == 63) {
             sh.wave_c[wave] = sc;
             sh.wave_w[wave] = sw;
+            if (kFar) sh.wave_h[wave] = su;
         }
         __syncthreads();
-        u64 ec = above_c + sc - sum_c, ew = above_w + sw - sum_w;
-#pragma unroll
-        for (int k = 0; k < kWaves; ++k) {
-            const u64 c_ = sh.wave_c[k], w_ = sh.wave_w[k];
-            ec += k < wave ? c_ : 0;
-            ew += k < wave ? w_ : 0;
+        u64 ec = above_c + sum_of_first(sh.wave_c, wave) + sc - sum_c, ew = above_w + sw - sum_w, eh = 0;
+        if (weights) {
+            ew += sum_of_first(sh.wave_w, wave);
+            if (kFar) eh = sum_of_first(sh.wave_h, wave) + su - sum_h;
+            if (kFar && p > 0.0)
+                goal = share_of(p, joined(sum_of_first(sh.wave_w, kWaves), sum_of_first(sh.wave_h, kWaves)));
         }
 #pragma unroll
         for (int i = 0; i < kOwn; ++i) {
-            const bool here = by_weight ? (double)ew < goal && (double)(ew + w[i]) >= goal
-                                        : ec < want && ec + c[i] >= want;
+            const bool here = !by_weight ? ec < want && ec + c[i] >= want
+                              : kFar     ? joined(ew, eh) < goal && joined(ew + w[i], eh + high[i]) >= goal
+                                         : ew < (u64)goal && ew + w[i] >= (u64)goal;
             if (here) {
                 sh.bin = kOwn * threadIdx.x + i;
                 sh.in_bin = c[i];
                 sh.above_c = ec;
-                sh.above_w = ew;
+                sh.above_w = kFar ? joined(ew, eh) : ew;
             }
             ec += c[i];
             ew += w[i];
+            eh += high[i];
         }
         __syncthreads();
+        return goal;
+    }
+    // What goal leaves to add, in units of that shift.
+    __device__ __forceinline__ u64 left_for(int shift, u128 goal, u128 above_w) const {
+        return (u64)((goal - above_w + (((u128)1 << shift) - 1)) >> shift);
     }
 
     // Place of the number-th entry (from 1) whose score is v, in index order.
@@ -923,27 +990,20 @@ struct Cutter {
         return r;
     }
 
-    // How many of `number` entries of the same score v the cut takes.
-    __device__ u64 equal_needed(X v, u64 number, bool by_weight, u64 want, double goal, u64 above_c, u64 above_w,
+    // How many of `number` entries of the same score v, of weight w, the cut takes.
+    __device__ u64 equal_needed(u64 w, u64 number, bool by_weight, u64 want, u64 goal, u64 above_c, u64 above_w,
                                 u64* up_to) const {
-        const u64 w = fixed_of(v);
-        u64 r;
-        if (by_weight) {
-            const double q = (goal - (double)above_w) / (double)w;  // w > 0: the weight reaches goal here
-            r = q < 1.0 ? 1 : q >= (double)number ? number : (u64)q;
-            while (r > 1 && (double)(above_w + (r - 1) * w) >= goal) --r;
-            while (r < number && (double)(above_w + r * w) < goal) ++r;
-        } else {
-            r = want - above_c;
-        }
+        u64 r = want - above_c;
+        if (by_weight) r = (goal - above_w + w - 1) / w;  // w > 0: the weight reaches goal here
+        r = r < number ? r : number;
         *up_to = above_w + r * w;
         return r;
     }
 
-    // The cut among the listed entries: split by the bits of their places until at most kRank are left, which
-    // are ranked.  Sums of whole numbers cross in every round; one that did not would leave in_bin 0 and end the loop.
-    __device__ u64 cut_list(uint32_t number, bool by_weight, u64 want, double goal, u64 above_c, u64 above_w,
-                            u64* up_to) {
+    // The cut among the listed entries, their weights in list_w: split by the bits of their places until at most kRank
+    // are left, which are ranked.  Sums of whole numbers cross in every round; one that did not would leave in_bin 0
+    // and end the loop.
+    __device__ u64 cut_list(uint32_t number, bool by_weight, u64 want, u64 goal, u64 above_c, u64 above_w, u64* up_to) {
         const int tid = threadIdx.x;
         u64 lo = 0, hi = ~(u64)0;  // places still in question
         if (tid == 0) sh.in_bin = number;
@@ -981,11 +1041,11 @@ struct Cutter {
                 if (weights) atomicAdd(&sh.weight[b], sh.list_w[i]);
             }
             __syncthreads();
-            cross(by_weight, want, goal, above_c, above_w);
-            above_c = sh.above_c;
-            above_w = sh.above_w;
+            cross<false>(by_weight, want, goal, above_c, above_w);
+            above_c = scalar(sh.above_c);
+            above_w = scalar((u64)sh.above_w);
             lo += (u64)sh.bin << shift;
-            const u64 span = ((u64)1 << shift) - 1;  // lo + span can pass 2^64: the lowest int32 scores' places end there
+            const u64 span = ((u64)1 << shift) - 1;  // lo + span can pass 2^64, where the lowest ints' places end
             hi = hi - lo > span ? lo + span : hi;
         }
         // at most kRank entries: each against all
@@ -1009,27 +1069,31 @@ struct Cutter {
                 before += earlier;
                 before_w += earlier ? other.y : 0;
             }
-            if (by_weight ? (double)before_w < goal && (double)(before_w + w) >= goal : before + 1 == want) {
+            if (by_weight ? before_w < goal && before_w + w >= goal : before + 1 == want) {
                 sh.found = p;
                 sh.found_w = before_w + w;
             }
         }
         __syncthreads();
-        const u64 r = sh.found;
-        *up_to = sh.found_w;
+        const u64 r = scalar(sh.found);
+        *up_to = scalar(sh.found_w);
         __syncthreads();
         return r;
     }
 
-    // The entry at which the count reaches want (by_weight false) or the weight reaches goal, in the order; the
-    // distance bins hold their sums.  *up_to: the weight up to and with it (where weights are summed).
-    __device__ u64 cut(bool by_weight, u64 want, double goal, u64* up_to) {
+    // The entry at which the count reaches want (by_weight false) or the weight reaches goal, or with p that share of
+    // all, in the order; the distance bins hold their sums.  *up_to: the weight up to and with it (where weights are
+    // summed).
+    __device__ u64 cut(bool by_weight, u64 want, u128 goal, double p, u128* up_to) {
         const int tid = threadIdx.x;
-        cross(by_weight, want, goal, 0, 0);
+        goal = cross<true>(by_weight, want, goal, 0, 0, p);
         uint32_t lo, hi;
-        keys_of(sh.bin, sh.bin, &lo, &hi);
+        const uint32_t bin = scalar(sh.bin);
+        u64 above_c = scalar(sh.above_c), above_w = 0, with = 0, at;  // from here on weights are of this bin's unit
+        const u128 far_w = scalar(sh.above_w);
+        const u64 need = by_weight ? left_for(shift_of(bin), goal, far_w) : 0;
+        keys_of(bin, bin, &lo, &hi);
         for (;;) {
-            const u64 above_c = sh.above_c, above_w = sh.above_w;
             __syncthreads();
             if (tid == 0) {
                 sh.listed = 0;
@@ -1066,12 +1130,16 @@ struct Cutter {
             hi = sh.hi;
             const uint32_t number = sh.listed;
             if (number <= kList) {
-                for (uint32_t i = tid; i < number; i += kLanes) sh.list_w[i] = fixed_of(S::value(key_at(sh.list[i])));
-                return cut_list(number, by_weight, want, goal, above_c, above_w, up_to);
+                for (uint32_t i = tid; i < number; i += kLanes)
+                    sh.list_w[i] = fixed_of(S::value(key_at(sh.list[i])), bin);
+                at = cut_list(number, by_weight, want, need, above_c, above_w, &with);
+                break;
             }
             if (lo == hi) {  // equal scores: as many of them as it takes, in index order
                 const X v = S::value(lo);
-                return nth_equal(v, equal_needed(v, number, by_weight, want, goal, above_c, above_w, up_to));
+                at = nth_equal(v, equal_needed(fixed_of(v, bin), number, by_weight, want, need, above_c, above_w,
+                                               &with));
+                break;
             }
             // split the range of keys: bins from the largest key down
             const int shift = 32 - __clz((hi - lo) >> kBinBits);
@@ -1083,30 +1151,33 @@ struct Cutter {
                     if (k < lo || k > hi) continue;
                     const uint32_t b = (hi - k) >> shift;
                     atomicAdd(&sh.count[b], 1u);
-                    if (weights) atomicAdd(&sh.weight[b], fixed_of(v[e]));
+                    if (weights) atomicAdd(&sh.weight[b], fixed_of(v[e], bin));
                 }
             });
             __syncthreads();
-            cross(by_weight, want, goal, above_c, above_w);
+            cross<false>(by_weight, want, need, above_c, above_w);
+            above_c = scalar(sh.above_c);
+            above_w = scalar((u64)sh.above_w);
             const uint32_t b = sh.bin, span = (1u << shift) - 1;
             hi -= b << shift;
             lo = hi - lo > span ? hi - span : lo;
         }
+        *up_to = far_w + ((u128)with << shift_of(bin));
+        return at;
     }
 
     // The last kept place by all filters.
     __device__ u64 last_kept(const Goal<S>& goal) {
-        u64 last = ~(u64)0, total = 0;
+        u64 last = ~(u64)0;
+        u128 total = 0;
 #pragma unroll 1
         for (int by_weight = goal.by_k ? 0 : 1; by_weight <= (goal.by_p ? 1 : 0); ++by_weight) {
             // top-k's cut first: top-p goes by the weight of the first k, and reaches its share of that before the last
             // of them
             if (!filled) fill_bins(goal.by_k && !by_weight);
-            if (by_weight && !goal.by_k) total = total_weight();
-            u64 up_to = 0;
-            const u64 at = cut(by_weight != 0, goal.k, goal.p * (double)total, &up_to);
+            const u64 at = cut(by_weight != 0, goal.k, share_of(goal.p, total),
+                               by_weight && !goal.by_k ? goal.p : 0.0, &total);
             last = at < last ? at : last;
-            total = up_to;
         }
         const u64 at = goal.last_by_weight();
         return at < last ? at : last;
@@ -1270,7 +1341,9 @@ struct SplitRow {
     uint32_t count[kBins];
     u64 weight[kBins];
     u64 list[2][kList];  // places: of top-k's bin, of top-p's
-    u64 above_c, above_w[2];  // before those bins: entries (top-k), weight
+    u128 above_w[2];  // before those bins: weight
+    u64 above_c;      // and entries (top-k)
+    u128 share;       // top-p's goal (without top-k)
     u64 last;                 // place of the last kept entry
     uint32_t listed[2], lo[2], hi[2];  // entries of those bins, their range of keys
     uint32_t found[2][kMaxSplits];     // entries of each split
@@ -1366,13 +1439,13 @@ __global__ void __launch_bounds__(kSplitLanes) gather_kernel(SampleArgs a, int s
     __syncthreads();
     // keys [lo, hi] of the bins of either cut; none: an empty range
     uint32_t lo[2] = {0xFFFFFFFFu, 0xFFFFFFFFu}, hi[2] = {0u, 0u};
-    u64 least = 0, most = 0;  // bounds of the first k's weight
+    u128 least = 0, most = 0;  // bounds of the first k's weight
     if (goal.by_k) {
-        cut.cross(false, goal.k, 0.0, 0, 0);
+        cut.template cross<true>(false, goal.k, 0, 0, 0);
         const uint32_t bin = sh.bin;
         cut.keys_of(bin, bin, &lo[0], &hi[0]);
         least = sh.above_w;
-        most = least + sh.weight[bin];
+        most = least + ((u128)sh.weight[bin] << cut.shift_of(bin));
         if (s == 0 && tid == 0) {
             w.above_c = sh.above_c;
             w.above_w[0] = least;
@@ -1380,17 +1453,15 @@ __global__ void __launch_bounds__(kSplitLanes) gather_kernel(SampleArgs a, int s
         __syncthreads();
     }
     if (goal.by_p) {
-        if (!goal.by_k) least = most = cut.total_weight();
-        // top-p's cut is between the goals that these bounds give (at least half a unit: a weight reaches it)
-        const double g = goal.p * (double)least;
-        cut.cross(true, 0, g < 0.5 ? 0.5 : g, 0, 0);
+        // after top-k its cut is between the goals that these bounds give (at least one unit: a weight reaches it)
+        const u128 share = cut.template cross<true>(true, 0, share_of(goal.p, least), 0, 0, goal.by_k ? 0.0 : goal.p);
         const uint32_t bin = sh.bin;
-        if (s == 0 && tid == 0) w.above_w[1] = sh.above_w;
-        __syncthreads();
-        if (goal.by_k) {
-            const double up = goal.p * (double)most;
-            cut.cross(true, 0, up < 0.5 ? 0.5 : up, 0, 0);
+        if (s == 0 && tid == 0) {
+            w.share = share;
+            w.above_w[1] = sh.above_w;
         }
+        __syncthreads();
+        if (goal.by_k) cut.template cross<true>(true, 0, share_of(goal.p, most), 0, 0);
         cut.keys_of(bin, sh.bin, &lo[1], &hi[1]);
         __syncthreads();
     }
@@ -1448,7 +1519,7 @@ __global__ void __launch_bounds__(kSplitLanes) gather_kernel(SampleArgs a, int s
 }
 
 template <int kType>
-__global__ void __launch_bounds__(kSplitLanes) sum_kernel(SampleArgs a, int splits, SplitRow* rows) {
+__global__ void __launch_bounds__(kSplitLanes, 4) sum_kernel(SampleArgs a, int splits, SplitRow* rows) {
     using S = Scores<kType>;
     using X = typename S::X;
     __shared__ CutShared<kSplitLanes> sh;
@@ -1461,42 +1532,61 @@ __global__ void __launch_bounds__(kSplitLanes) sum_kernel(SampleArgs a, int spli
     const Region mine(row.groups, splits * kSplitWaves, region);
     Cutter<kSplitLanes, S> cut(row, mine, goal, sh);
     const u64 q = goal.last_by_weight();
-    u64 last = q, total = 0;
+    u64 last = q;
+    u128 share = w.share;  // top-k's cut has another
     int writer = 0;  // the split that knows the row's last place: all do, but of equal scores
 #pragma unroll 1
     for (int c = goal.by_k ? 0 : 1; c <= (goal.by_p ? 1 : 0); ++c) {
-        if (c && !goal.by_k) {
+        uint32_t number = w.listed[c], bin = cut.bin_of(S::value(w.lo[c]));
+        const u64 above_c = c ? 0 : w.above_c;
+        u128 above_w = w.above_w[c];
+        // Top-p's list after top-k's cut is of all bins that the cut can be in: where their units are further apart
+        // than the sums have bits for, those of the cut's own bin are ranked.
+        const bool several = c && goal.by_k && number <= kList &&
+                             cut.shift_of(cut.bin_of(S::value(w.hi[c]))) > cut.shift_of(bin) + 1;
+        if (several) {
             for (int b = tid; b < kBins; b += kSplitLanes) sh.weight[b] = w.weight[b];
             __syncthreads();
-            total = cut.total_weight();
+            cut.template cross<true>(true, 0, share, 0, 0);
+            bin = scalar(sh.bin);
+            above_w = scalar(sh.above_w);
+            if (tid == 0) sh.listed = 0;
+            __syncthreads();
         }
-        const uint32_t number = w.listed[c];
-        const double share = goal.p * (double)total;
-        const u64 above_c = c ? 0 : w.above_c, above_w = w.above_w[c];
-        u64 up_to = 0, at;
+        const int shift = cut.shift_of(bin);
+        const u64 need = c ? cut.left_for(shift, share, above_w) : 0;
+        u64 with = 0, at;
         if (number <= kList) {
             for (uint32_t k = tid; k < number; k += kSplitLanes) {
                 const u64 p = w.list[c][k];
-                sh.list[k] = p;
-                sh.list_w[k] = cut.fixed_of(S::value(key_at(p)));
+                const X v = S::value(key_at(p));
+                const uint32_t own = cut.bin_of(v);
+                if (several && own != bin) continue;
+                const uint32_t to = several ? atomicAdd(&sh.listed, 1u) : k;
+                sh.list[to] = p;
+                sh.list_w[to] = cut.fixed_of(v, own) << (cut.shift_of(own) - shift);
             }
-            at = cut.cut_list(number, c != 0, goal.k, share, above_c, above_w, &up_to);
+            if (several) {
+                __syncthreads();
+                number = sh.listed;
+            }
+            at = cut.cut_list(number, c != 0, goal.k, need, above_c, 0, &with);
             writer = 0;
         } else {
             // the earlier splits keep all of these, the later ones none
             const uint32_t key = w.lo[c];
             const X v = S::value(key);
-            const u64 need = cut.equal_needed(v, number, c != 0, goal.k, share, above_c, above_w, &up_to);
+            const u64 taken = cut.equal_needed(cut.fixed_of(v, bin), number, c != 0, goal.k, need, above_c, 0, &with);
             const int lane = tid & 63;  // kMaxSplits lanes
             const uint32_t here = lane < splits ? w.found[c][lane] : 0;
             const u64 to = wave_scan((u64)here);
-            const int split = __ffsll(__ballot(to >= need)) - 1;
+            const int split = __ffsll(__ballot(to >= taken)) - 1;
             at = place_of(key, s < split ? 0xFFFFFFFFu : 0u);
-            if (s == split) at = cut.nth_equal(v, need - (u64)__shfl(to - here, split, 64));
+            if (s == split) at = cut.nth_equal(v, taken - (u64)__shfl(to - here, split, 64));
             writer = q < place_of(key, 0u) ? 0 : split;
         }
         last = at < last ? at : last;
-        total = up_to;
+        share = share_of(goal.p, above_w + ((u128)with << shift));
     }
     if (s == writer && tid == 0) w.last = last;
     const Part p = sum_kept(row, mine, Kept<S>(last), goal);

@@ -446,3 +446,105 @@ def test_the_lowest_ints_after_one_far_above(torch):
                 dict(T=T, k=None, p=(0.999 * k / 502).astype(np.float32), q=None)):
         say(f"sample lowest int32 after one {[n for n in 'Tkpq' if par[n] is not None]}")
         check(torch, x, bits(rng, len(k)), par, "lowest int32 after one")
+
+
+def flat_tail(N, peak, D, T0, p, draw):
+    """(T, kept, pick, logp) of a row with one score of 0, at index peak, and N - 1 of -D: w = exp(-D / T) each, top-p.
+    T is the first of some float32 numbers from T0 up whose cut is not near a border between two entries."""
+    p = np.longdouble(np.float32(p))
+    for i in range(100):
+        T = np.float32(T0 * (1 + i * 2.0 ** -20))
+        w = np.exp(-np.longdouble(D) / np.longdouble(T))
+        n = (p * (1 + (N - 1) * w) - 1) / w  # entries of the tail that reach p
+        if 0.25 < n - np.floor(n) < 0.75 and 0 < n < N - 2:
+            break
+    else:
+        raise AssertionError("no such T")
+    n = int(np.ceil(n))
+    S = 1 + n * w
+    t = np.longdouble(int(draw) >> 11) * np.longdouble(2.0) ** -53 * S
+    if t < min(peak, n) * w:
+        return T, n + 1, int(t / w), float(np.log(w / S))
+    if t < min(peak, n) * w + 1:
+        return T, n + 1, peak, float(-np.log(S))
+    return T, n + 1, int((t - 1) / w) + 1, float(np.log(w / S))
+
+
+@pytest.mark.parametrize("name", TYPES)
+@pytest.mark.parametrize("R,N,D,T,p", [
+    (1, 1 << 18, 29, 1.0, 1 - 2.0 ** -24), (200, 1 << 18, 29, 1.0, 1 - 2.0 ** -24), (2, 1 << 18, 16, 0.75, 0.9999),
+    (3, 1 << 20, 30, 1.0, 1 - 2.0 ** -24), (200, 1 << 20, 27, 0.99, 0.999999), (2, 1 << 24, 27, 0.99, 0.99999)])
+def test_flat_tails(torch, name, R, N, D, T, p):
+    """A peak and a long tail of equal scores, each of a weight that is small beside the peak's and much together: the
+    count is the tail's, not that of a tail whose weights were rounded (a weight is off by 2^-38 of itself at most, the
+    count by less than 0.001 and the pick by less than 0.01; T keeps the cut a quarter away from a border)."""
+    scale = 1000 if name == "i32" else 1
+    peak = N // 3
+    row = torch.full((1, N), -D * scale, dtype=dtype(torch, name), device="cuda")
+    row[0, peak] = 0
+    draws = np.array([0, 0x8000000000000000, 0xFFFFFFFFFFFFF800], np.uint64)[np.arange(R) % 3]
+    want = [flat_tail(N, peak, D * scale, T * scale, p, d) for d in draws[:3]]
+    out = hx.SampleBuffers.empty(R, N)
+    for k in (None, N - 1):
+        say(f"sample flat tail {name} {R} x {N} D={D} p={p} k={k}")
+        if k:  # without the last entry, and p of what is left: one entry of N fewer
+            want = [flat_tail(N - 1, peak, D * scale, T * scale, p, d) for d in draws[:3]]
+        par = dict(T=np.full(R, want[0][0], np.float32), k=None if k is None else np.full(R, k, np.int32),
+                   p=np.full(R, p, np.float32), q=None)
+        hx.sample(row.expand(R, N), device_draws(torch, draws), out, device_params(torch, par))
+        torch.cuda.synchronize()
+        each = [np.resize(np.array([v[i] for v in want]), R) for i in (2, 3, 1)]
+        compare(out, (each[0].astype(np.int32), each[1], each[2].astype(np.int32)), "flat tail")
+
+
+@pytest.mark.parametrize("name", ["i32", "f16"])
+def test_longest_flat_tail(torch, name):
+    """The same at HX_MAX_COLS (a weight off by 2^-32 of itself at most, the count by 0.15)."""
+    N, peak = 1 << 30, 12345
+    scale = 1000 if name == "i32" else 1
+    x = torch.full((1, N), -23 * scale, dtype=dtype(torch, name), device="cuda")
+    x[0, peak] = 0
+    draws = np.array([0x1000000000000000], np.uint64)
+    out = hx.SampleBuffers.empty(1, N)
+    T, kept, pick, logp = flat_tail(N, peak, 23 * scale, scale, 0.95, draws[0])
+    say(f"sample flat tail {name} 1 x {N} kept {kept}")
+    hx.sample(x, device_draws(torch, draws), out,
+              device_params(torch, dict(T=np.full(1, T, np.float32), k=None, p=np.full(1, 0.95, np.float32), q=None)))
+    torch.cuda.synchronize()
+    compare(out, (np.array([pick], np.int32), np.array([logp]), np.array([kept], np.int32)), "longest flat tail")
+
+
+@pytest.mark.parametrize("name", ["i32", "f32"])
+@pytest.mark.parametrize("R,N", [(2, 30000), (2, 262144), (70, 30000)])
+def test_spread_tails(torch, name, R, N):
+    """A peak and a tail of different scores past the distance bins' range, most of them in the last bin."""
+    rng = np.random.default_rng([64, R, N])
+    x = -rng.uniform(24.5, 28.0, (R, N))
+    x[:, N // 2] = 0
+    x = (x * 1e6).astype(np.int32) if name == "i32" else x.astype(np.float32)
+    T = np.full(R, 1e6 if name == "i32" else 1.0, np.float32)
+    dev = torch.as_tensor(x).to("cuda")
+    for p in (1 - 2.0 ** -24, 1 - 2.0 ** -23, 1 - 2.0 ** -20):
+        for k in (None, np.full(R, N // 2, np.int32)):
+            say(f"sample spread tail {name} {R} x {N} p={p}")
+            check(torch, dev, bits(rng, R), dict(T=T, k=k, p=np.full(R, p, np.float32), q=None), "spread tail")
+
+
+@pytest.mark.parametrize("name", TYPES)
+@pytest.mark.parametrize("N", [3000, 30000])
+def test_few_far_apart(torch, name, N):
+    """Top-k of a few scores far apart and top-p among them: bounds of the first k's weight that many bins lie
+    between."""
+    rng = np.random.default_rng([65, N])
+    R = 12
+    x = rng.uniform(-60, -30, (R, N))
+    gaps = np.array([0.0, 1.5, 3.0, 5.0, 8.0, 13.0, 21.0])
+    for r in range(R):
+        x[r, rng.permutation(N)[:len(gaps)]] = -gaps * rng.uniform(0.8, 1.2)
+    scale = 1000 if name == "i32" else 1
+    dev = torch.as_tensor(x * scale).to("cuda").to(dtype(torch, name))
+    T = np.full(R, scale, np.float32)
+    for p in (0.8, 0.9, 0.95, 0.99, 0.999, 0.99999):
+        k = rng.integers(2, 9, R).astype(np.int32)
+        say(f"sample far apart {name} N={N} p={p}")
+        check(torch, dev, bits(rng, R), dict(T=T, k=k, p=np.full(R, p, np.float32), q=None), f"far apart {name}")
