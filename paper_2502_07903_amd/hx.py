@@ -740,7 +740,8 @@ class Dispatcher:
     hold its tokens.  A decode replica has the blocks of the bmax requests of mean length
     (s_in + s_out) that Table 1's memory limit admits.  Replica j of `pool` is decode node j of
     `ws.net`; row i of `rows` is request i.  After `create` (which reads the placement's replicas
-    back once) no call synchronises."""
+    back once) no call synchronises.  The calls change the dispatcher's buffers, so those on one
+    stream have to be ordered after those on another by the caller."""
     placement: DeviceProblem
     ws: Workspace
     routes: RouteBuffers
@@ -757,7 +758,8 @@ class Dispatcher:
     def create(cls, dp: DeviceProblem, cand: int, n_rows: int, max_tokens: int, max_slots: int, block_size: int = 16,
                device: str = "cuda", stream=None) -> "Dispatcher":
         """For column cand of dp (replica networks: granularity 0), n_rows requests of at most max_tokens tokens
-        each, and at most max_slots new tokens in one call."""
+        each, and at most max_slots new tokens in one call.  On a stream of its own it comes after what the
+        current stream of that GPU holds, and that stream's later work after it."""
         torch = _torch()
         if dp.space.granularity != 0:
             raise ValueError("requests are dispatched to replicas: granularity 0")
@@ -766,7 +768,8 @@ class Dispatcher:
         if not 0 <= cand < dp.cand.n_cand:
             raise ValueError(f"column {cand} of a batch of {dp.cand.n_cand}")
         if stream is not None:
-            stream.wait_stream(torch.cuda.current_stream())  # what dp's tensors still wait for
+            callers = torch.cuda.current_stream(stream.device)
+            stream.wait_stream(callers)  # what dp's tensors still wait for
         with torch.cuda.stream(stream):
             one = dp.with_candidates(dp.tensors["assign"][:, cand:cand + 1].clone(),
                                      dp.tensors["role"][:, cand:cand + 1].clone())
@@ -783,9 +786,12 @@ class Dispatcher:
             rows = KvRows.empty(n_rows, width, device)
             rows.replica = routes.decode
             rows.replica.fill_(-1)
-            return cls(one, ws, routes, KvPool.create(blocks, block_size, device), rows, z(n_rows + 1, torch.int64),
+            made = cls(one, ws, routes, KvPool.create(blocks, block_size, device), rows, z(n_rows + 1, torch.int64),
                        z(max_slots, torch.int64), z(n_rows, torch.uint8), kv_workspace(n_rows, len(blocks), device),
                        z(n_rows, torch.int32, 1), z(n_rows, torch.uint8, 1))
+        if stream is not None:
+            callers.wait_stream(stream)  # the fills of its buffers
+        return made
 
     def admit(self, rnd, prompt, stream=None) -> None:
         """A request in every row, over whatever the rows held: routed by its draw (rnd, int64 bit patterns), its

@@ -184,3 +184,38 @@ def test_dispatcher_refuses_columns(torch, cand):
     dp = hx.DeviceProblem.upload(I.make_problem(1, n_cand=2))
     with pytest.raises(ValueError):
         hx.Dispatcher.create(dp, cand, 4, 16, 64)
+
+
+def test_dispatcher_created_on_another_stream_and_used_at_once(torch, monkeypatch):
+    """create(stream=side) with work between the fills of its buffers, and the first calls on the current stream
+    straight after it: they come after the fills."""
+    dp = hx.DeviceProblem.upload(I.make_problem(1, n_cand=64))
+    want = hx.Dispatcher.create(dp, 5, 40, 64, 40 * 64)
+    rnd = torch.arange(40, device="cuda", dtype=torch.int64) * 0x0123456789ABCDEF
+    prompt = torch.full((40,), 3, dtype=torch.int32, device="cuda")
+    busy = torch.zeros(1 << 26, device="cuda")
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    real = hx.kv_workspace
+
+    def slow(*args, **kw):
+        assert torch.cuda.current_stream() == side
+        for _ in range(200):
+            busy.add_(1.0)
+        return real(*args, **kw)
+    monkeypatch.setattr(hx, "kv_workspace", slow)
+    got = hx.Dispatcher.create(dp, 5, 40, 64, 40 * 64, stream=side)
+    after = torch.cuda.Event()
+    after.record()
+    got.admit(rnd, prompt)
+    got.step()
+    after.synchronize()
+    assert side.query()  # what the current stream has reached comes after all of the other's work
+    want.admit(rnd, prompt)
+    want.step()
+    torch.cuda.synchronize()
+    assert busy[0] == 200 and (got.all_rows == 1).all()
+    for a, b in ((want.rows.held, got.rows.held), (want.rows.table, got.rows.table), (want.slots, got.slots),
+                 (want.tok_base, got.tok_base), (want.placed, got.placed), (want.one, got.one),
+                 (want.pool.free_count, got.pool.free_count), (want.routes.decode, got.routes.decode)):
+        assert torch.equal(a, b)
