@@ -543,8 +543,9 @@ int hx_kv_place(const hx_kv_pool *pool, const hx_kv_rows *rows, const int32_t *n
 
 /* The blocks of every row with done[i] != 0 back to its replica, held_out 0 there: the last row's last block
  * first, so that releasing the rows that one hx_kv_place served on empty caches leaves the free lists as they
- * were.  Tables keep their entries.  Rows on no replica, with held negative or past max_blocks columns, or
- * whose blocks would not fit the replica's range, are left alone. */
+ * were.  Tables keep their entries.  Rows on no replica, and with held negative or past max_blocks columns, are
+ * left alone.  Rows of one replica are released in descending order until the first whose blocks would not fit
+ * the replica's range, which is left alone, and from there only rows that hold no blocks. */
 int hx_kv_release(const hx_kv_pool *pool, const hx_kv_rows *rows, const uint8_t *done, void *workspace,
                   size_t workspace_bytes, hipStream_t stream);
 

@@ -192,3 +192,13 @@ def test_pool_refuses():
         hx.KvPool.create([], 16, device="cpu")
     with pytest.raises(ValueError):
         hx.KvPool.create([3, -1], 16, device="cpu")
+
+
+def test_plain_release_stops_at_the_first_that_does_not_fit():
+    # replica 0 has room for two blocks, replica 1 for two: from the last row down, row 3 takes one of replica 0's,
+    # row 2 needs two and closes it, row 0 would fit but comes after it; row 4's blocks go to replica 1
+    base, free_list = np.array([0, 4, 6]), np.array([0, 1, -1, -1, -1, -1])
+    table = np.array([[5, -1], [-1, -1], [6, 7], [8, -1], [3, 4]])
+    held, left = O.release(2, base, free_list, np.array([2, 0]), table, 2, [0, 0, 0, 0, 1], [2, 0, 3, 1, 4], [1] * 5)
+    assert held.tolist() == [2, 0, 3, 0, 0] and left.tolist() == [3, 2]
+    assert free_list.tolist() == [0, 1, 8, -1, 4, 3]

@@ -378,3 +378,18 @@ def test_refuses(torch):
             f()
     with pytest.raises(hx.HxError):
         hx.route_requests(net, flow, d, out, cand=1)
+
+
+@pytest.mark.parametrize("rows", [5, 1500])
+def test_release_stops_at_the_first_that_does_not_fit(torch, rows):
+    """A large row that does not fit among small ones that would, before and after it, on two replicas."""
+    m = Memory(torch, [3 * rows, 3 * rows], 2, rows, 4)
+    m.set(replica=np.arange(rows) % 2)
+    m.place(np.full(rows, 2))
+    held = np.full(rows, 2)
+    held[rows // 2] = 8
+    m.set(held=held, table=np.arange((rows + 2) * 4).reshape(rows + 2, 4),
+          free=[3 * rows - rows // 4 - 2, 3 * rows - 1])
+    say(f"kv release of a row that does not fit: {rows}")
+    m.release(np.ones(rows), tag="one does not fit")
+    assert 0 < (m.h["held"] > 0).sum() < rows and m.h["held"][rows // 2] == 8
