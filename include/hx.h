@@ -529,7 +529,7 @@ typedef struct hx_kv_rows {
  * only rows that need none.  The row that is served takes the top of its replica's free list, block by
  * block, into its next table columns; its token t gets slot block * b + (held + t) mod b.
  *   tok_base [n_rows + 1]: sum of n_new over the rows before (a negative n_new counts 0);
- *   slots  [max_slots]: row i's tokens at tok_base[i]; -1 for those of a row not served; entries past the
+ *   slots  [max_slots], at most 2^35 - 2048: row i's tokens at tok_base[i]; -1 for those of a row not served; entries past the
  *          last token are left as they were;
  *   placed [n_rows]: 1 where served, held_out = held + n_new there and held elsewhere.
  * Not served: rows on no replica, with held or n_new negative, past max_blocks columns or 2^31 - 1 tokens,

@@ -591,6 +591,7 @@ int hx_kv_place(const hx_kv_pool* pool, const hx_kv_rows* rows, const int32_t* n
     int rc = check_kv(pool, rows, workspace, workspace_bytes);
     if (rc) return rc;
     if (!n_new || !tok_base || !placed || max_slots < 0 || (max_slots > 0 && !slots)) return HX_EINVAL;
+    if (max_slots > hx::kMaxSlots) return HX_EINVAL;
     hipError_t e = hx::launch_place(*pool, *rows, n_new, tok_base, slots, max_slots, placed, workspace, stream);
     return e == hipSuccess ? HX_OK : hip_error(e);
 }

@@ -699,7 +699,7 @@ hipError_t launch_place(const hx_kv_pool& p, const hx_kv_rows& r, const int32_t*
         hipLaunchKernelGGL((kv_rows_kernel<true, false>), dim3(a.chunks), dim3(kLanes), 0, s, a, 0);
     }
     if (!fill) {
-        // a grid has fewer than 2^32 lanes: up to 2^35 slots, whose 256 GiB are most of the memory
+        static_assert(kMaxSlots / kFillTokens * kFillLanes < (int64_t)1 << 32, "a grid's lanes");
         const int64_t fills = (max_slots + kFillTokens - 1) / kFillTokens;
         hipLaunchKernelGGL(place_fill_kernel, dim3((unsigned)(fills < 1 ? 1 : fills)), dim3(kFillLanes), 0, s, a);
     }

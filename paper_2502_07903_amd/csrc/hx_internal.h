@@ -203,6 +203,7 @@ size_t route_workspace_bytes(int32_t max_p, int32_t max_d, int32_t max_pd, int32
 hipError_t launch_route(const FlowNet& f, int32_t cand, const int32_t* kv_flow, const uint64_t* rnd, const hx_routes& o,
                         void* workspace, hipStream_t s);
 size_t kv_workspace_bytes(int32_t n_rows, int32_t n_replicas);
+constexpr int64_t kMaxSlots = ((int64_t)1 << 35) - 2048;  // of a call: its grid has fewer than 2^32 lanes
 hipError_t launch_place(const hx_kv_pool& p, const hx_kv_rows& r, const int32_t* n_new, int64_t* tok_base,
                         int64_t* slots, int64_t max_slots, uint8_t* placed, void* workspace, hipStream_t s);
 hipError_t launch_release(const hx_kv_pool& p, const hx_kv_rows& r, const uint8_t* done, void* workspace,

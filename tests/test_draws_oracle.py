@@ -202,3 +202,9 @@ def test_plain_release_stops_at_the_first_that_does_not_fit():
     held, left = O.release(2, base, free_list, np.array([2, 0]), table, 2, [0, 0, 0, 0, 1], [2, 0, 3, 1, 4], [1] * 5)
     assert held.tolist() == [2, 0, 3, 0, 0] and left.tolist() == [3, 2]
     assert free_list.tolist() == [0, 1, 8, -1, 4, 3]
+
+
+@pytest.mark.parametrize("slots", [(1 << 35) - 2047, 1 << 43, (1 << 43) + 2048, (1 << 63) - 1])
+def test_place_refuses_more_slots_than_a_grid_has(slots):
+    """Before anything is launched: no row is served, and no block taken."""
+    assert _kv(False, lambda a: a.update(max_slots=slots)) == hx.HX_EINVAL
