@@ -426,10 +426,10 @@ __device__ int target_region(double mine, double u, bool one, double* sum, doubl
 }
 
 // The first entry of groups [lo, hi) up to which the weights sum to more than t, or the last one with weight
-// (which rounding can leave as the only choice), to the row's outputs.  weights(entries, index of the first, w): 0 for
-// entries that are not kept.  Every lane of the workgroup calls it; some entry has weight.
+// (which rounding can leave as the only choice), to the row's outputs; false if none has weight.  weights(entries, index
+// of the first, w): 0 for entries that are not kept.  Every lane of the workgroup calls it.
 template <int kLanes, class S, class W>
-__device__ void pick_in_region(const Row<S>& row, const Region& g, double t, const Draw& draw, W weights,
+__device__ bool pick_in_region(const Row<S>& row, const Region& g, double t, const Draw& draw, W weights,
                                PickShared<kLanes>& sh) {
     constexpr int kWaves = kLanes / 64;
     const int wave = wave_index(), lane = threadIdx.x & 63;
@@ -485,11 +485,13 @@ __device__ void pick_in_region(const Row<S>& row, const Region& g, double t, con
                     if (e == e_found) value = (double)v[e];
                 draw.write(row.first(at) + e_found, value);
             }
-            return;
+            return true;
         }
         __syncthreads();
     }
+    if (last < 0) return false;
     if (threadIdx.x == 0) draw.write(last, (double)S::widen(row.x[last]));
+    return true;
 }
 
 // ------------------------------------------------------------------ no filters
@@ -607,10 +609,19 @@ __device__ void finish_row(const SampleArgs& a, int64_t r, const Row<S>& row, co
     }
     const double u = (double)(a.rnd[r] >> 11) * 0x1p-53;
     double sum, before;
-    const int target = target_region<kLanes>(mine, u, false, &sum, &before, sh);
-    pick_in_region<kLanes>(
-        row, Region(row.groups, regions, target), u * sum - before, Draw{a, r, (double)top, (double)par.T, sum, count},
-        [&](const X (&v)[S::V], int, double (&w)[S::V]) { ex.weights(v, w); }, sh);
+    int target = target_region<kLanes>(mine, u, false, &sum, &before, sh);
+    const Draw draw{a, r, (double)top, (double)par.T, sum, count};
+    const auto weights = [&](const X (&v)[S::V], int, double (&w)[S::V]) { ex.weights(v, w); };
+    double t = u * sum - before;
+    while (!pick_in_region<kLanes>(row, Region(row.groups, regions, target), t, draw, weights, sh)) {
+        // Entries that weigh 0 each and something together, where t is an earlier region's end but for rounding: the next
+        // region with weight, or behind the last the last entry of a region whose entries do weigh something.
+        double all, ahead;
+        const bool next = __syncthreads_or((int)threadIdx.x > target && mine > 0.0);
+        const double in = next ? ((int)threadIdx.x > target ? mine : 0.0) : (mine >= 0x1p-900 ? mine : 0.0);
+        target = target_region<kLanes>(in, next ? 0.0 : 2.0, next, &all, &ahead, sh);
+        t = next ? 0.0 : INFINITY;
+    }
 }
 
 // A row's split s of `splits`: workgroup r * splits + s.  With one split the row ends here.

@@ -548,3 +548,41 @@ def test_few_far_apart(torch, name, N):
         k = rng.integers(2, 9, R).astype(np.int32)
         say(f"sample far apart {name} N={N} p={p}")
         check(torch, dev, bits(rng, R), dict(T=T, k=k, p=np.full(R, p, np.float32), q=None), f"far apart {name}")
+
+
+FULL = (1 << 64) - 1
+
+
+def deep_rows(R, N, name):
+    """Rows (of 20,000 entries, each 27 regions of 768 where one workgroup has the row) whose last regions hold weights
+    that are 0 each and, relative to the first scores of the same wavefront's regions, something together."""
+    rng = np.random.default_rng([66, R, N])
+    x = rng.uniform(-5, 0, (R, N))
+    x[:, 24 * 768:24 * 768 + 256] = -40
+    x[:, 25 * 768:] = -748.5
+    return (x * (1 << 20)).astype(np.int32) if name == "i32" else x.astype(np.float32)
+
+
+@pytest.mark.parametrize("name", ["f32", "i32"])
+@pytest.mark.parametrize("R", [1, 300, 2000])
+def test_draws_at_the_end_of_the_weights(torch, name, R):
+    """The largest draws: each falls to an entry with weight, next to the place at which its share of the weights ends
+    (sums rounded in another order: 20,000 terms, off by 2^-53 of the sum for each at most)."""
+    N, T = 20000, float(1 << 20) if name == "i32" else 1.0
+    x = deep_rows(R, N, name)
+    draws = np.array([FULL, FULL - 0x800, FULL - 0x1000, FULL - 0x4000], np.uint64)[np.arange(R) % 4]
+    out = hx.SampleBuffers.empty(R, N)
+    say(f"sample end of the weights {name} {R} x {N}")
+    hx.sample(torch.as_tensor(x).to("cuda"), device_draws(torch, draws), out,
+              device_params(torch, dict(T=np.full(R, T, np.float32), k=None, p=None, q=None)))
+    torch.cuda.synchronize()
+    pick, logp = out.pick.cpu().numpy(), out.logp.cpu().numpy()
+    assert (out.kept == N).all() and (pick >= 0).all()
+    for r in range(R):
+        z = (x[r].astype(np.float64) - x[r].max()) / T
+        w = np.exp(z)
+        run = np.cumsum(w.astype(np.longdouble))
+        t, eps = (int(draws[r]) >> 11) * np.longdouble(2.0) ** -53 * run[-1], N * 2.0 ** -53 * run[-1]
+        assert w[pick[r]] > 0 and run[pick[r]] > t - eps and run[pick[r]] - w[pick[r]] <= t + eps
+        want = z[pick[r]] - float(np.log(run[-1]))
+        assert abs(logp[r] - want) <= abs(want) * 2.0 ** -24 * 1.001 + 1e-11
