@@ -601,12 +601,15 @@ __device__ void finish_row(const SampleArgs& a, int64_t r, const Row<S>& row, co
         return;
     }
     Exponent ex;
-    ex.set(top, par.scale());
     double mine = 0.0;
     if ((int)threadIdx.x < regions) {
+        // by half the exponent twice: a part's weight can be up to 2^524, and its score's 0
         const Part p = parts[threadIdx.x];
-        mine = p.count ? p.weight * ex.weight(S::value(p.key)) : 0.0;
+        ex.set(top, 0.5 * par.scale());
+        const double half = p.count ? ex.weight(S::value(p.key)) : 0.0;
+        mine = p.weight * half * half;
     }
+    ex.set(top, par.scale());
     const double u = (double)(a.rnd[r] >> 11) * 0x1p-53;
     double sum, before;
     int target = target_region<kLanes>(mine, u, false, &sum, &before, sh);
@@ -614,8 +617,8 @@ __device__ void finish_row(const SampleArgs& a, int64_t r, const Row<S>& row, co
     const auto weights = [&](const X (&v)[S::V], int, double (&w)[S::V]) { ex.weights(v, w); };
     double t = u * sum - before;
     while (!pick_in_region<kLanes>(row, Region(row.groups, regions, target), t, draw, weights, sh)) {
-        // Entries that weigh 0 each and something together, where t is an earlier region's end but for rounding: the next
-        // region with weight, or behind the last the last entry of a region whose entries do weigh something.
+        // Entries that weigh 0 each and something together, where t is 0 or an earlier region's end but for rounding: the
+        // next region with weight, or behind the last the last entry of a region whose entries do weigh something.
         double all, ahead;
         const bool next = __syncthreads_or((int)threadIdx.x > target && mine > 0.0);
         const double in = next ? ((int)threadIdx.x > target ? mine : 0.0) : (mine >= 0x1p-900 ? mine : 0.0);

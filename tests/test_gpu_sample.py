@@ -586,3 +586,22 @@ def test_draws_at_the_end_of_the_weights(torch, name, R):
         assert w[pick[r]] > 0 and run[pick[r]] > t - eps and run[pick[r]] - w[pick[r]] <= t + eps
         want = z[pick[r]] - float(np.log(run[-1]))
         assert abs(logp[r] - want) <= abs(want) * 2.0 ** -24 * 1.001 + 1e-11
+
+
+@pytest.mark.parametrize("R,N", [(1, 20000), (1, 700000), (300, 20000), (600, 3000)])
+def test_the_smallest_draw(torch, R, N):
+    """Draws of 0 fall to the first entry that weighs anything: scores far below the others' first, 700 T below them
+    next (weights of 2^-1010), at several places of a region and of the row."""
+    rng = np.random.default_rng([67, R, N])
+    x = rng.uniform(-5, 0, (R, N))
+    for r in range(R):
+        first = int(rng.choice([1, 100, 300, 500, 1000, N // 3, N // 2, N - 1000]))
+        x[r, :first] = rng.choice([-1000.0, -3000.0, -np.inf])
+        x[r, first:first + 400] = np.where(np.arange(min(400, N - first)) % 7 == 3, -700.0, -900.0)
+    x = x.astype(np.float32)
+    say(f"sample smallest draws {R} x {N}")
+    dev = torch.as_tensor(x).to("cuda")
+    for draws in (np.zeros(R, np.uint64), np.full(R, 0x7FF, np.uint64)):
+        check(torch, dev, draws, dict(T=np.ones(R, np.float32), k=None, p=None, q=None), "smallest draw")
+        check(torch, dev, draws, dict(T=np.ones(R, np.float32), k=np.full(R, N - 5, np.int32), p=None, q=None),
+              "smallest draw of the first k")
