@@ -503,12 +503,12 @@ constexpr int kAllRegions = 8, kShortRow = 8192;
 constexpr int kFinishLanes = 256;
 constexpr int kMaxSplits = 64;
 
-// The largest of the lanes' entries.
+// The largest of the lanes' entries.  Cleaned first: of a signalling NaN and a number the maximum is NaN.
 template <class S>
 __device__ __forceinline__ typename S::X wave_most(const typename S::X (&v)[S::V]) {
     typename S::X most = S::kMasked;
 #pragma unroll
-    for (int e = 0; e < S::V; ++e) most = S::larger(most, v[e]);
+    for (int e = 0; e < S::V; ++e) most = S::larger(most, S::clean(v[e]));
     return wave_max(most);
 }
 
@@ -615,16 +615,16 @@ __device__ void finish_row(const SampleArgs& a, int64_t r, const Row<S>& row, co
     int target = target_region<kLanes>(mine, u, false, &sum, &before, sh);
     const Draw draw{a, r, (double)top, (double)par.T, sum, count};
     const auto weights = [&](const X (&v)[S::V], int, double (&w)[S::V]) { ex.weights(v, w); };
-    double t = u * sum - before;
-    while (!pick_in_region<kLanes>(row, Region(row.groups, regions, target), t, draw, weights, sh)) {
-        // Entries that weigh 0 each and something together, where t is 0 or an earlier region's end but for rounding: the
-        // next region with weight, or behind the last the last entry of a region whose entries do weigh something.
-        double all, ahead;
-        const bool next = __syncthreads_or((int)threadIdx.x > target && mine > 0.0);
-        const double in = next ? ((int)threadIdx.x > target ? mine : 0.0) : (mine >= 0x1p-900 ? mine : 0.0);
-        target = target_region<kLanes>(in, next ? 0.0 : 2.0, next, &all, &ahead, sh);
-        t = next ? 0.0 : INFINITY;
+    if (pick_in_region<kLanes>(row, Region(row.groups, regions, target), u * sum - before, draw, weights, sh)) return;
+    // Entries that weigh 0 each and something together, where the draw is 0 or an earlier region's end but for rounding:
+    // the next region with weight, or behind the last the last entry of a region whose entries do weigh something.
+    double all, ahead;
+    while (__syncthreads_or((int)threadIdx.x > target && mine > 0.0)) {
+        target = target_region<kLanes>((int)threadIdx.x > target ? mine : 0.0, 0.0, true, &all, &ahead, sh);
+        if (pick_in_region<kLanes>(row, Region(row.groups, regions, target), 0.0, draw, weights, sh)) return;
     }
+    target = target_region<kLanes>(mine >= 0x1p-900 ? mine : 0.0, 2.0, false, &all, &ahead, sh);
+    pick_in_region<kLanes>(row, Region(row.groups, regions, target), INFINITY, draw, weights, sh);
 }
 
 // A row's split s of `splits`: workgroup r * splits + s.  With one split the row ends here.

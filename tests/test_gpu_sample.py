@@ -605,3 +605,25 @@ def test_the_smallest_draw(torch, R, N):
         check(torch, dev, draws, dict(T=np.ones(R, np.float32), k=None, p=None, q=None), "smallest draw")
         check(torch, dev, draws, dict(T=np.ones(R, np.float32), k=np.full(R, N - 5, np.int32), p=None, q=None),
               "smallest draw of the first k")
+
+
+@pytest.mark.parametrize("N", [900, 9000, 40000])
+@pytest.mark.parametrize("name", ("f32", "f16", "bf16"))
+def test_every_nan_is_masked(torch, name, N):
+    """Signalling and quiet, of either sign, with the smallest and the largest payloads."""
+    rng = np.random.default_rng([68, N])
+    R = 5
+    x = torch.as_tensor(scores(rng, name, R, N)).to("cuda").to(dtype(torch, name))
+    word, inf = (torch.int32, 0x7F800000) if name == "f32" else (torch.int16, 0x7C00 if name == "f16" else 0x7F80)
+    quiet = 0x00400000 if name == "f32" else 0x0200 if name == "f16" else 0x0040
+    sign = -(1 << 31) if name == "f32" else -(1 << 15)
+    kinds = [inf + 1, inf + quiet, inf + 2 * quiet - 1, inf + quiet - 1]
+    kinds += [k + sign for k in kinds]
+    where = rng.random((R, N)) < np.array([0.01, 0.2, 0.9, 0.5, 1.0])[:, None]
+    values = torch.as_tensor(rng.choice(kinds, (R, N))).to("cuda").to(word)
+    x.view(word).copy_(torch.where(torch.as_tensor(where).to("cuda"), values, x.view(word)))
+    assert torch.equal(torch.isnan(x.cpu()), torch.as_tensor(where))
+    for which in ("", "k", "p", "kpq"):
+        say(f"sample NaN {name} N={N} '{which}'")
+        check(torch, x, bits(rng, R), params(rng, R, which), f"NaN {name}")
+    check(torch, x, bits(rng, R), dict(T=np.zeros(R, np.float32), k=None, p=None, q=None), f"NaN {name}")
