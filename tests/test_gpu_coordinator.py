@@ -219,3 +219,46 @@ def test_dispatcher_created_on_another_stream_and_used_at_once(torch, monkeypatc
                  (want.tok_base, got.tok_base), (want.placed, got.placed), (want.one, got.one),
                  (want.pool.free_count, got.pool.free_count), (want.routes.decode, got.routes.decode)):
         assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("cfg,n_rows,most,bs", [(1, 4000, 3000, 16), (1, 3, 100, 16), (2, 700, 2000, 7), (3, 900, 4096, 64)])
+def test_dispatcher_pool_and_slots(torch, cfg, n_rows, most, bs):
+    """A decode replica's blocks are those of bmax requests of mean length, or all that the rows can take; the rest of
+    the pool is empty; and no two placed tokens of a replica get the same slot, over prompts and a step."""
+    rng = np.random.default_rng([54, cfg, n_rows])
+    prob = I.make_problem(cfg, n_cand=64)
+    value = hxo.score_batch(prob)["flow_value"]
+    dp = hx.DeviceProblem.upload(prob)
+    d = hx.Dispatcher.create(dp, int(value.argmax()), n_rows, most, n_rows * most, block_size=bs)
+    n_d = int(d.ws.net.n_d[0])
+    bmax = d.ws.cost.bmax[:, 0].cpu().numpy().astype(np.int64)[d.ws.net.d_slot[:n_d, 0].cpu().numpy()]
+    wl = dp.workload
+    per_request = int(np.ceil(np.ceil(wl.s_in + wl.s_out) / bs))
+    width = int(np.ceil(most / bs))
+    blocks = np.diff(d.pool.base.cpu().numpy().astype(np.int64))
+    want = np.minimum(bmax * per_request, n_rows * width)
+    say(f"dispatcher pool: workload {cfg}, {n_rows} rows, blocks {want.tolist()}")
+    assert n_d > 0 and want.max() > 0
+    assert blocks[:n_d].tolist() == want.tolist() and not blocks[n_d:].any()
+    assert d.pool.free_count.cpu().numpy().tolist() == blocks.tolist()
+    assert d.rows.table.shape == (n_rows, width)
+    lens = rng.integers(1, most, n_rows).astype(np.int32)
+    taken = []
+    for step in range(2):
+        if step:
+            d.step()
+            new = (before > 0).astype(np.int64)
+        else:
+            d.admit(draws_of(torch, rng, n_rows)[1], torch.as_tensor(lens).to("cuda"))
+            new = lens.astype(np.int64)
+        placed, slots = d.placed.cpu().numpy(), d.slots.cpu().numpy()
+        row = np.repeat(np.arange(n_rows), new)
+        mine = slots[:len(row)]
+        assert ((mine >= 0) == (placed[row] == 1)).all() and d.tok_base.cpu().numpy()[-1] == len(row)
+        replica = d.routes.decode.cpu().numpy()[row]
+        ok = mine >= 0
+        assert (mine[ok] < blocks[replica[ok]] * bs).all()
+        taken.append(np.stack([replica[ok], mine[ok]], 1))
+        before = d.rows.held.cpu().numpy()
+    taken = np.concatenate(taken)
+    assert len(taken) == before.sum() > 0 and len(np.unique(taken, axis=0)) == len(taken)
