@@ -627,3 +627,23 @@ def test_every_nan_is_masked(torch, name, N):
         say(f"sample NaN {name} N={N} '{which}'")
         check(torch, x, bits(rng, R), params(rng, R, which), f"NaN {name}")
     check(torch, x, bits(rng, R), dict(T=np.zeros(R, np.float32), k=None, p=None, q=None), f"NaN {name}")
+
+
+@pytest.mark.parametrize("which", ["", "kp"])
+def test_more_rows_than_a_launch(torch, which):
+    """2^20 + 5 rows of the same scores; some of them, at both ends of either launch, against the plain version."""
+    R, N = (1 << 20) + 5, 37
+    rng = np.random.default_rng(69)
+    x = torch.as_tensor(scores(rng, "f32", 1, N)).to("cuda").expand(R, N)
+    draws, par = bits(rng, R), params(rng, R, which)
+    out = hx.SampleBuffers.empty(R, N)
+    for t in (out.pick, out.kept):
+        t.fill_(0x55)
+    say(f"sample {R} rows '{which}'")
+    hx.sample(x, device_draws(torch, draws), out, device_params(torch, par))
+    torch.cuda.synchronize()
+    some = np.r_[0:40, 1000:1040, (1 << 20) - 40:R]
+    host = np.repeat(x[:1].cpu().numpy(), len(some), 0)
+    want = O.sample(host, draws[some], *(None if par[k] is None else par[k][some] for k in "Tkpq"))
+    compare(hx.SampleBuffers(out.pick[some], out.logp[some], out.kept[some], None), want, "many rows")
+    assert int(out.pick.min()) >= 0 and int(out.pick.max()) < N and int(out.kept.min()) >= 1
