@@ -628,7 +628,7 @@ __device__ void finish_row(const SampleArgs& a, int64_t r, const Row<S>& row, co
 }
 
 // A row's split s of `splits`: workgroup r * splits + s.  With one split the row ends here.
-// Bound by the exponentials' binary64 operations, 27 vector instructions an entry in all: 1,024 rows of 131,072 bf16
+// Bound by the exponentials' binary64 operations, 26 vector instructions an entry in all: 1,024 rows of 131,072 bf16
 // 112 us a call, 2.4 TB/s, of which reading the 268 MB once is 52 us; a row of 256 i32 4.4 us, the launch.
 template <int kType>
 __global__ void __launch_bounds__(kAllLanes) all_kernel(SampleArgs a, int splits, Part* parts) {
@@ -1322,7 +1322,7 @@ __device__ void cut_row(const SampleArgs& a, int64_t r, const Row<S>& row, const
 }
 
 // 256 rows of 50,257 f16 with top-p and min-p: 77 us, of which a row takes 4 for its extent, 22 for the bins' weights
-// (an exponential and two LDS atomics an entry), 7 to 25 for the cut, 8 for the kept entries' sums and 4 for the draw.
+// (an exponential and an LDS atomic of 64 bits an entry), 7 to 25 for the cut, 8 for the kept entries' sums and 4 for the draw.
 // The later passes find the row in the caches; every pass ends in a barrier that waits for the slowest wavefront.
 template <int kType>
 __global__ void __launch_bounds__(kCutLanes, 4) cut_kernel(SampleArgs a) {  // four wavefronts a SIMD: 128 registers
@@ -1341,7 +1341,7 @@ __global__ void __launch_bounds__(kCutLanes, 4) cut_kernel(SampleArgs a) {  // f
 //   gather_kernel  the entries of the bins in which the cuts fall, into the row's lists
 //   sum_kernel     the cuts, from the lists; weight and number of the regions' kept entries
 //   draw_kernel    a workgroup per row: the draw
-// 16 rows of 131,072 i32 with top-p: 4.5, 8.5, 10.5, 13.5 and 6 us.  Each launch is bound by its chain: the first
+// 16 rows of 131,072 i32 with top-p: 4.5, 8.5, 10.5, 13 and 6 us.  Each launch is bound by its chain: the first
 // loads, the row's state from the other workgroups, one pass over 4,096 entries or more, the reduction.
 // The draw as the last step of the row's last workgroup of sum_kernel, a device-wide fence in each, takes 104 us
 // instead of 42.
@@ -1646,10 +1646,11 @@ constexpr int32_t kSplitRows = 192;  // of more rows none is split
 
 // Workgroups a row with filters is split into, 4,096 entries or more to each; 0: one workgroup and a single launch.
 // Splitting takes five launches, in which every split works out the row's cuts for itself, and pays while the rows
-// alone leave most of the chip idle: 16 rows of 131,072 i32 with top-p 42 against 150 us, 64 of 32,768 41 against 48,
-// 192 of 131,072 f32 with top-k and top-p 129 against 162, one of 8,388,608 124 against 6,586; but one of 16,384 27
-// against 22, 128 of 32,768 56 against 49, 260 of 131,072 215 against 192, 512 of 262,144 1,297 against 572.  Where a
-// row's lists overflow, which rows of a million float scores can, it costs a quarter more: 64 rows 1,681 against 1,452.
+// alone leave most of the chip idle: 16 rows of 131,072 i32 with top-p 43 against 154 us, 64 of 32,768 41 against 50,
+// 192 of 131,072 f32 with top-k and top-p 133 against 164, one of 8,388,608 121 against 7,825; but one of 16,384 27
+// against 22, 128 of 32,768 56 against 49, 260 of 131,072 215 against 192, 512 of 262,144 1,297 against 572.  Where
+// more scores than a list holds share the bin of a cut, not all equal, it costs an eighth more: 16 rows of 262,144 f32
+// with top-p 442 against 389, 64 of 1,048,576 1,805 against 1,593.
 int cut_splits_of(int32_t R, int32_t N) {
     if (N < 24576 || R > kSplitRows || (int64_t)R * 500 > N) return 0;
     int64_t s = 1024 / R, most = N / 4096;
