@@ -706,6 +706,7 @@ def dispatch_main(args, torch, hx, I):
                    "decode_replicas": int(d.ws.net.n_d[0]), "kv_blocks": int(d.pool.base[-1])},
         "best": best,
         "requests_served": held,
+        "note": "value counts every request of a step; requests_served of them found KV memory",
         "kernel_us": {k: 1000.0 * v / c for k, (v, c) in prof.items() if c > 0},
     }))
 
