@@ -464,8 +464,8 @@ typedef struct hx_sampling {
  *   entry, in ascending index, up to which the kept weights sum to more than t.
  * Every sum is taken in binary64 or, where top-p's cut is looked for, in whole numbers, in an order that does
  * not depend on the launch's timing.  For the whole numbers a weight is rounded by at most 1.03 2^-51 of itself,
- * past 1,024 columns 1.03 2^(ceil(log2 N) - 62) of itself (2^-45 at 131,072, 2^-32 at 2^30); weights below e^-24,
- * and all at T < 2^-122, by no more than that times e^-24 (times 1).
+ * past 1,024 columns 1.03 2^(ceil(log2 N) - 62) of itself (2^-45 at 131,072, 2^-32 at 2^30).  A weight below e^-24
+ * is off by no more than one of e^-24 can be; where T < 2^-117, any weight by no more than one of 1.
  *   rnd  [R] uniform 64-bit draws;
  *   pick [R] the index drawn; logp [R] nullable: z_pick - log S; kept [R] nullable: min(K, P, Q).
  * T = 0 gives the argmax, logp 0, kept 1.  A row that masks everything, or whose T is negative or not
